@@ -449,6 +449,192 @@ int reflex_profile_graph(reflex_ctx* ctx, const float* state, const float* noise
                          const float* tau_schedule, float* actions_out, uint32_t class_mask, int32_t reps,
                          double* ms_per_replay, int32_t* launches);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Backbone operators: rotary positions, the paged cache and its attention
+ * ---------------------------------------------------------------------------
+ *
+ * The cache above takes pre-RoPE K/V of its prefix and frames from a
+ * vision-language backbone.  These calls are what such a backbone runs to
+ * produce them: rotary positions over several axes, a paged K/V cache that may
+ * hold 8-bit values, and the attention of a chunk of new tokens over it.  They
+ * need no reflex_ctx.
+ *
+ * Memory and streams: every buffer belongs to the caller; nothing is allocated
+ * and no call waits for the device.  Work is enqueued on `stream` (a
+ * hipStream_t, NULL = the null stream) of the current device, on which every
+ * buffer has to lie; it may be captured into a HIP graph, which then reads the
+ * device arrays (lengths, page table, positions) anew at every replay.  The
+ * host structs are read during the call only.  The calls keep no state, so
+ * several threads may make them at once.
+ *
+ * Element types: `dtype` (REFLEX_DTYPE_*) is the type of queries, keys, values
+ * and results outside the cache.  All arithmetic is fp32 or wider; results are
+ * rounded once.
+ */
+
+/* Packed rows of heads: element (row r, head h, d) at data[r*row_stride +
+ * h*head_stride + d], strides in elements.  data is 16-byte aligned and the
+ * strides are multiples of 16 bytes.  Rows of an output must not overlap. */
+typedef struct reflex_rows {
+  void* data;
+  int64_t row_stride;
+  int64_t head_stride;
+} reflex_rows;
+
+/* How the frequencies of a rotary plan fall: with REFLEX_LADDER_SHARED pair i
+ * of head_dim/2 turns by theta^(-i / (head_dim/2)) per position whichever axis
+ * it follows; with REFLEX_LADDER_PER_AXIS the j-th of an axis's m pairs turns
+ * by theta^(-j / m). */
+#define REFLEX_LADDER_SHARED 0
+#define REFLEX_LADDER_PER_AXIS 1
+
+#define REFLEX_MAX_AXES 4
+#define REFLEX_MAX_PAIRS 128
+
+/* A rotary plan (host memory, filled by reflex_rotary_init, read-only after). */
+typedef struct reflex_rotary {
+  int32_t head_dim;
+  int32_t n_axes;
+  uint8_t axis[REFLEX_MAX_PAIRS];   /* the axis that pair i follows */
+  double turns[REFLEX_MAX_PAIRS];   /* full turns of pair i per position */
+} reflex_rotary;
+
+/*
+ * Fill a rotary plan (pure host function).  Pair i is dimensions i and
+ * i + head_dim/2 of a head (rotate-half, as in the action expert).  The first
+ * sections[0] pairs follow axis 0, the next sections[1] axis 1, and so on (for
+ * image tokens: time, height, width); their sum is head_dim/2.  One axis with
+ * the shared ladder is the rotary embedding of the action expert.
+ * head_dim: a multiple of 16 from 16 to 256.  Errors: REFLEX_EINVAL.
+ */
+int reflex_rotary_init(reflex_rotary* plan, int32_t head_dim, int32_t n_axes, const int32_t* sections, double theta,
+                       int32_t ladder);
+
+/*
+ * Rotate n_rows rows of n_heads heads by their positions: y[i] = x[i] cos(a) -
+ * x[i + half] sin(a), y[i + half] = x[i + half] cos(a) + x[i] sin(a) with a the
+ * pair's angle at the row's position on the pair's axis.  inverse != 0 turns
+ * the other way: the gradient of the rotation, and what gives a rotated key
+ * its pre-RoPE values back.
+ * positions: device int64, row r's position on axis a at [a*pos_stride + r].
+ * Angles are reduced in 64 bits; |position| < 2^40.
+ * y may be x (the same data and strides); otherwise they must not overlap.
+ * n_rows: at most 2^27, in this call and in those below; 0 does nothing.
+ * Errors: REFLEX_EINVAL, REFLEX_EHIP.
+ */
+int reflex_rotary_apply(const reflex_rotary* plan, const int64_t* positions, int64_t pos_stride, const reflex_rows* x,
+                        const reflex_rows* y, int64_t n_rows, int32_t n_heads, int32_t dtype, int32_t inverse,
+                        void* stream);
+
+/* Element types of the pages.  F32 and BF16 pages hold the inputs' own type.
+ * FP8 (e4m3) and INT8 pages hold, per token and K/V head, head_dim codes and
+ * one fp32 scale; a value is code * scale.
+ *   INT8: scale = max|x| * (1/127) (fp32 product with the fp32 nearest 1/127; at
+ *         least 2^-126), code = x / scale to nearest.
+ *   FP8:  scale = the smallest power of two (at least 2^-126) with max|x| <=
+ *         448 * scale, code = x / scale to nearest.
+ * Ties go to the even code.  What lies next to a border is decided exactly: K
+ * is rotated and divided in 64 bits.  A row with an infinity or a NaN gets the
+ * scale NaN: all of it reads as NaN. */
+#define REFLEX_STORE_F32 0
+#define REFLEX_STORE_BF16 1
+#define REFLEX_STORE_FP8 2
+#define REFLEX_STORE_INT8 3
+
+/*
+ * A paged cache: n_pages pages of page_size tokens.
+ *   k, v              [n_pages][n_kv_heads][page_size][head_dim], 16-byte aligned
+ *   k_scale, v_scale  [n_pages][n_kv_heads][page_size] fp32 (8-bit stores; else NULL)
+ * page_size: a power of two from 1 to 1024; head_dim: 64, 128 or 256;
+ * n_pages * n_kv_heads * page_size < 2^31.
+ */
+typedef struct reflex_paged_cache {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t store;      /* REFLEX_STORE_* */
+  int32_t reserved;
+} reflex_paged_cache;
+
+/*
+ * Which tokens a call is about (device int32 arrays).  Sequence b has
+ * lengths[b] tokens, the last n_b = cu_rows[b+1] - cu_rows[b] of which are the
+ * call's rows cu_rows[b] .. cu_rows[b+1] - 1, oldest first.  Token p of the
+ * sequence lies in slot p % page_size of page page_table[b][p / page_size].
+ * Rows outside [cu_rows[0], cu_rows[n_seqs]) belong to no sequence: they are
+ * not read, and what an output holds there stays.
+ * A table entry outside [0, n_pages), and every token beyond max_pages pages
+ * or before the sequence's start, is absent: nothing is written for it, it
+ * reads as zeros and no query sees it.  Sequences may share pages that a call
+ * only reads; of two rows of one write for the same slot either may win.
+ * cu_rows is non-decreasing from a value >= 0; what exceeds the call's n_rows
+ * is cut off there.
+ * max_length: the length that the longest sequence is expected to reach (0:
+ * max_pages * page_size).  It only sizes the launch: longer ones stay correct.
+ */
+typedef struct reflex_paged_batch {
+  const int32_t* cu_rows;     /* [n_seqs + 1] */
+  const int32_t* lengths;     /* [n_seqs] */
+  const int32_t* page_table;  /* [n_seqs][max_pages] */
+  int32_t n_seqs;
+  int32_t max_pages;
+  int32_t max_length;
+  int32_t reserved;
+} reflex_paged_batch;
+
+/*
+ * Write K and V of the batch's rows ([n_rows][n_kv_heads][head_dim], dtype)
+ * into their pages.  With a rotary plan (may be NULL) the keys are rotated
+ * first, by `positions` as in reflex_rotary_apply, or, with positions NULL, by
+ * the token's index in its sequence on every axis.
+ * Errors: REFLEX_EINVAL; REFLEX_EDTYPE where an F32 or BF16 store differs from
+ * dtype; REFLEX_EHIP.
+ */
+int reflex_paged_write(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const reflex_rows* k,
+                       const reflex_rows* v, int64_t n_rows, int32_t dtype, const reflex_rotary* rotary,
+                       const int64_t* positions, int64_t pos_stride, void* stream);
+
+/*
+ * Read K and V of the batch's rows back: code * scale, rounded to dtype.  A
+ * batch whose n_b is lengths[b] reads whole sequences.  Keys come as they were
+ * written; reflex_rotary_apply with inverse gives their pre-RoPE values, which
+ * is what reflex_cache_init and reflex_cache_write_frame take.
+ * Errors: as reflex_paged_write.
+ */
+int reflex_paged_read(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const reflex_rows* k,
+                      const reflex_rows* v, int64_t n_rows, int32_t dtype, void* stream);
+
+/*
+ * Attention of the batch's rows over the pages of their sequences, which hold
+ * the rows' own K/V already:
+ *   out[r][h] = sum_j softmax_j(scale * q[r][h] . k[j][g]) v[j][g],
+ * g = h / (n_q_heads / n_kv_heads), over the keys j that row r sees.  With p
+ * the row's token index in its sequence (rows are the last n_b tokens) and L
+ * the sequence's length, these are the present tokens j < L, with causal != 0
+ * only j <= p, and with window > 0 only j > p - window.  A row that sees none
+ * gets zeros.
+ * Keys that a row does not see have no part in its result, whatever they hold
+ * (NaN and infinities included).  Probabilities enter the second product in
+ * dtype, all sums are fp32; results do not depend on what else is on the GPU.
+ * q, out: [n_rows][n_q_heads][head_dim], not overlapping.  n_q_heads: a
+ * multiple of n_kv_heads; n_rows * n_q_heads <= 2^25.
+ * workspace: at least the bytes that reflex_paged_attention_workspace gives
+ * (which may be 0), 256-byte aligned; private to the call until its work is
+ * done.
+ * Errors: as reflex_paged_write.
+ */
+int reflex_paged_attention_workspace(const reflex_paged_cache* cache, const reflex_paged_batch* batch, int64_t n_rows,
+                                     int32_t n_q_heads, int32_t dtype, size_t* bytes);
+int reflex_paged_attention(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const reflex_rows* q,
+                           const reflex_rows* out, int64_t n_rows, int32_t n_q_heads, int32_t dtype, float scale,
+                           int32_t causal, int32_t window, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -17,6 +17,9 @@ struct LaunchEvents {
 };
 extern thread_local LaunchEvents g_launch_events;
 
+// Keeps the text of a HIP error for reflex_strerror; returns REFLEX_EHIP.
+int hip_fail(hipError_t e);
+
 #define RFX_LAUNCH(kernel, grid, block, shm, stream, ...)                                            \
   hipExtLaunchKernelGGL(kernel, grid, block, shm, stream, ::reflex::g_launch_events.start,          \
                         ::reflex::g_launch_events.stop, 0, __VA_ARGS__)

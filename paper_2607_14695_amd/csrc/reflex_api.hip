@@ -257,12 +257,14 @@ struct reflex_ctx {
   std::vector<hipEvent_t> pipe_free;
 };
 
-namespace {
-
+namespace reflex {
 int hip_fail(hipError_t e) {
   snprintf(g_hip_err, sizeof(g_hip_err), "HIP error %d: %s", (int)e, hipGetErrorString(e));
   return REFLEX_EHIP;
 }
+}  // namespace reflex
+
+namespace {
 
 // Ring bookkeeping of writing frame f (Section 3.1 FIFO; Appendix B.2).  A
 // ring with a spare slot places frame f in slot f mod (W + 1).
@@ -1210,7 +1212,7 @@ const char* reflex_strerror(int status) {
   switch (status) {
     case REFLEX_OK: return "ok";
     case REFLEX_EINVAL: return "invalid argument or unsupported configuration";
-    case REFLEX_EDTYPE: return "weight dtype does not match the configured compute dtype";
+    case REFLEX_EDTYPE: return "element type of the weights or of the pages does not match the compute dtype";
     case REFLEX_EHIP: return g_hip_err[0] ? g_hip_err : "HIP error";
     case REFLEX_ESTATE: return "context not initialised or destroyed";
     case REFLEX_ENONFINITE: return "a denoise produced a non-finite action since the last status check";

@@ -39,6 +39,12 @@ MODE_NAIVE = 2
 MODE_UNFUSED = 3
 MODES = {"reflex": MODE_REFLEX, "standard": MODE_STANDARD, "naive": MODE_NAIVE, "unfused": MODE_UNFUSED}
 NORM_PRECISIONS = {"fp32": 0, "bf16": 1, "bf16_fp32_stats": 2}
+STORE_F32 = 0
+STORE_BF16 = 1
+STORE_FP8 = 2
+STORE_INT8 = 3
+MAX_PAIRS = 128
+LADDERS = {"shared": 0, "per_axis": 1}
 ATTN_KERNELS = {"auto": 0, "rows16": 1, "pair": 2, "rows16p": 3}
 
 c_i32, c_i64, c_f32, c_f64, c_vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_double, ctypes.c_void_p
@@ -79,6 +85,29 @@ class SourcesC(ctypes.Structure):
     ]
 
 
+class RowsC(ctypes.Structure):
+    _fields_ = [("data", c_vp), ("row_stride", c_i64), ("head_stride", c_i64)]
+
+
+class RotaryC(ctypes.Structure):
+    _fields_ = [("head_dim", c_i32), ("n_axes", c_i32), ("axis", ctypes.c_uint8 * MAX_PAIRS),
+                ("turns", c_f64 * MAX_PAIRS)]
+
+
+class PagedCacheC(ctypes.Structure):
+    _fields_ = [
+        ("k", c_vp), ("v", c_vp), ("k_scale", c_vp), ("v_scale", c_vp), ("n_pages", c_i32), ("page_size", c_i32),
+        ("n_kv_heads", c_i32), ("head_dim", c_i32), ("store", c_i32), ("reserved", c_i32),
+    ]
+
+
+class PagedBatchC(ctypes.Structure):
+    _fields_ = [
+        ("cu_rows", c_vp), ("lengths", c_vp), ("page_table", c_vp), ("n_seqs", c_i32), ("max_pages", c_i32),
+        ("max_length", c_i32), ("reserved", c_i32),
+    ]
+
+
 class ReflexError(RuntimeError):
     def __init__(self, status: int, what: str, text: str):
         super().__init__(f"{what} failed with status {status}: {text}")
@@ -116,6 +145,15 @@ def load_library() -> ctypes.CDLL:
         "reflex_profile_read": (c_i32, [c_vp, P(ctypes.c_char_p), P(c_f64), P(c_i32), P(c_i32)]),
         "reflex_profile_graph": (c_i32, [c_vp, c_vp, c_vp, c_i32, c_vp, c_vp, ctypes.c_uint32, c_i32, P(c_f64),
                                          P(c_i32)]),
+        "reflex_rotary_init": (c_i32, [P(RotaryC), c_i32, c_i32, P(c_i32), c_f64, c_i32]),
+        "reflex_rotary_apply": (c_i32, [P(RotaryC), c_vp, c_i64, P(RowsC), P(RowsC), c_i64, c_i32, c_i32, c_i32, c_vp]),
+        "reflex_paged_write": (c_i32, [P(PagedCacheC), P(PagedBatchC), P(RowsC), P(RowsC), c_i64, c_i32, P(RotaryC),
+                                       c_vp, c_i64, c_vp]),
+        "reflex_paged_read": (c_i32, [P(PagedCacheC), P(PagedBatchC), P(RowsC), P(RowsC), c_i64, c_i32, c_vp]),
+        "reflex_paged_attention_workspace": (c_i32, [P(PagedCacheC), P(PagedBatchC), c_i64, c_i32, c_i32,
+                                                     P(ctypes.c_size_t)]),
+        "reflex_paged_attention": (c_i32, [P(PagedCacheC), P(PagedBatchC), P(RowsC), P(RowsC), c_i64, c_i32, c_i32,
+                                           c_f32, c_i32, c_i32, c_vp, ctypes.c_size_t, c_vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)

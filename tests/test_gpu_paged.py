@@ -1,0 +1,530 @@
+"""GPU parity of the backbone operators against their float64 definitions.
+
+Tolerances.  One rounding to a type is off by at most half a step: 2^-8 of the value in bf16, 2^-24 in fp32.
+* rotary: the result's rounding, and in fp32 the sine, the cosine and three operations on |a| + |b| (8 * 2^-24).
+* pages of 8 bits hold the definition's codes and scales exactly; bf16 and fp32 pages are rotary results.
+* attention: a score's fp32 products and sums move it by (dh + 4) 2^-24 of `reach` (the row's largest scale *
+  sum |q||k|), so its probability by that share, and so does the maximum; exp2 and the probability's own sums add
+  2^-21 and a step for each of the keys' partial sums, at most 2^-24 * 64 as they are taken in trees; in bf16 the
+  probability is rounded once (2^-8).  All of it weighs on `spread` = sum p|v|, and the sum of the probabilities
+  doubles it.  Then the result's own rounding.
+"""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_14695_amd import reflex as R
+from paper_2607_14695_amd.paged import PagedBatch, PagedCache, Rotary
+
+from . import paged_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+ROUND = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+CODE = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.float8_e4m3fn, "int8": torch.int8}
+
+
+def draw(gen, shape, dtype):
+    return torch.randn(shape, generator=gen).to(DT[dtype])
+
+
+def f64(t):
+    return t.detach().float().cpu().double().numpy() if t.dtype != torch.float64 else t.cpu().numpy()
+
+
+def pool(news, lengths, ps, gen, spare=3, more_pages=0):
+    """(cu, lengths, table, pages): every sequence's pages drawn from one shuffled pool."""
+    need = [-(-max(n, 0) // ps) for n in lengths]
+    n_pages = sum(need) + spare
+    order = torch.randperm(n_pages, generator=gen).to(torch.int32)
+    table = torch.full((len(lengths), max(need + [1]) + more_pages), -1, dtype=torch.int32)
+    at = 0
+    for b, m in enumerate(need):
+        table[b, :m] = order[at:at + m]
+        at += m
+    cu = torch.tensor([0] + list(news)).cumsum(0).to(torch.int32)
+    return cu, torch.tensor(lengths, dtype=torch.int32), table, n_pages
+
+
+def batch(cu, lengths, table, max_length=0):
+    return PagedBatch(cu.to(DEV), lengths.to(DEV), table.to(DEV), max_length)
+
+
+def filled(n_pages, hk, ps, dh, store, gen):
+    """(cache, values of K, values of V): every slot filled, in 8 bits by the definition's encoder."""
+    sides, values = [], []
+    for strong in (True, False):
+        x = torch.randn(n_pages, hk, ps, dh, generator=gen)
+        if strong:
+            x *= torch.exp(0.5 * torch.randn(hk, 1, dh, generator=gen))
+        if store in ("f32", "bf16"):
+            sides.append((x.to(CODE[store]).to(DEV), None))
+            values.append(f64(x.to(CODE[store])))
+            continue
+        scale = torch.exp2(torch.randint(-6, 3, (n_pages, hk, ps), generator=gen).float()) * 1.25
+        if store == "int8":
+            code = torch.randint(-127, 128, x.shape, generator=gen).to(torch.int8)
+            scale /= 64
+        else:
+            code = (x * 4).to(torch.float8_e4m3fn)
+        sides.append((code.to(DEV), scale.to(DEV)))
+        values.append(f64(code.float()) * f64(scale)[..., None])
+    (k, ks), (v, vs) = sides
+    return PagedCache(k, v, ks, vs), values[0], values[1]
+
+
+# ---------------------------------------------------------------------------
+# rotary
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,heads,dh,sections,ladder,far", [
+    (1, 1, 64, (32,), "shared", 0), (3, 8, 256, (32, 48, 48), "shared", 10 ** 9), (257, 5, 80, (13, 27), "per_axis", 5000),
+    (61, 2, 16, (8,), "shared", 100), (40, 33, 96, (0, 20, 20, 8), "per_axis", 10 ** 6), (5000, 3, 128, (16, 24, 24), "shared", 0)])
+def test_rotary(n, heads, dh, sections, ladder, far, dtype):
+    gen = torch.Generator().manual_seed(n * dh)
+    x = draw(gen, (n, heads, dh), dtype)
+    pos = torch.randint(-3, 4096, (len(sections), n), generator=gen) + far
+    rot = Rotary(dh, sections, theta=10000.0, ladder=ladder)
+    ang = ref.rotary_angles(pos.numpy(), sections, 10000.0, ladder, dh // 2)
+    for inverse in (False, True):
+        got = f64(rot.apply(x.to(DEV), pos.to(DEV), inverse=inverse))
+        want = ref.rotate(f64(x), ang, inverse)
+        half = dh // 2
+        both = np.abs(f64(x)[..., :half]) + np.abs(f64(x)[..., half:])
+        both = np.concatenate([both, both], -1)
+        # the angle itself: 64-bit products of positions up to 10^9
+        tol = ROUND[dtype] * np.abs(want) + both * (8 * 2.0 ** -24 + 4 * 2.0 ** -53 * (far + 5000))
+        assert np.all(np.abs(got - want) <= tol)
+
+
+def test_rotary_strides_in_place_and_gradient():
+    """A slice of packed rows, written into another slice; in place; one set of positions for all axes; and the
+    inverse as the gradient of the rotation, against differences."""
+    gen = torch.Generator().manual_seed(5)
+    n, heads, dh = 37, 4, 64
+    packed = torch.randn(n, 3 * heads * dh, generator=gen)
+    pos = torch.randint(0, 1000, (n,), generator=gen)
+    rot = Rotary(dh, (12, 20))
+    want = ref.rotate(f64(packed).reshape(n, 3 * heads, dh)[:, heads:2 * heads],
+                      ref.rotary_angles(pos.numpy(), (12, 20), 10000.0, "shared", 32))
+    dev = packed.to(DEV)
+    x = dev.view(n, 3 * heads, dh)[:, heads:2 * heads]
+    out = dev.view(n, 3 * heads, dh)[:, 2 * heads:]
+    assert rot.apply(x, pos.to(DEV), out=out) is out
+    np.testing.assert_allclose(f64(out), want, atol=4e-6)
+    rot.apply(x, pos.to(DEV), out=x)
+    np.testing.assert_allclose(f64(x), want, atol=4e-6)
+    assert torch.equal(dev[:, :heads * dh].cpu(), packed[:, :heads * dh])
+    # L = sum w . rotate(x); dL/dx = inverse rotation of w, and (L(x + e) - L(x - e)) / 2e along a direction
+    w, d = torch.randn(n, heads, dh, generator=gen), torch.randn(n, heads, dh, generator=gen)
+    x0 = torch.randn(n, heads, dh, generator=gen)
+    grad = f64(rot.apply(w.to(DEV), pos.to(DEV), inverse=True))
+    ang = ref.rotary_angles(pos.numpy(), (12, 20), 10000.0, "shared", 32)
+    loss = lambda t: float((f64(w) * ref.rotate(t, ang)).sum())  # noqa: E731
+    e = 1e-4
+    diff = (loss(f64(x0) + e * f64(d)) - loss(f64(x0) - e * f64(d))) / (2 * e)
+    assert abs(diff - float((grad * f64(d)).sum())) <= 1e-5 * float(np.abs(grad * f64(d)).sum())
+
+
+# ---------------------------------------------------------------------------
+# write and read
+# ---------------------------------------------------------------------------
+SEQS = {
+    "one": ([1], [1]),
+    "tokens": ([1] * 9, [1, 5, 16, 17, 40, 3, 8, 9, 33]),
+    "ragged": ([0, 7, 33, 0, 0, 1, 130], [3, 7, 50, 0, 1, 20, 131]),
+    "many_empty": ([0] * 70 + [3] + [0] * 130 + [2, 1], [4] * 203),
+    "cut_off": ([5, 4], [3, 4]),  # more rows than tokens: the first two lie before the sequence's start
+}
+
+
+@pytest.mark.parametrize("seqs", sorted(SEQS))
+@pytest.mark.parametrize("dtype,store,hk,dh,ps", [
+    ("bf16", "bf16", 1, 256, 16), ("bf16", "fp8", 2, 128, 8), ("bf16", "int8", 3, 64, 1), ("f32", "f32", 2, 64, 128),
+    ("f32", "fp8", 1, 64, 32), ("f32", "int8", 5, 256, 4)])
+def test_write_then_read(seqs, dtype, store, hk, dh, ps):
+    news, lengths = SEQS[seqs]
+    gen = torch.Generator().manual_seed(dh + ps)
+    cu, lens, table, n_pages = pool(news, lengths, ps, gen)
+    n = int(cu[-1])
+    k = draw(gen, (n + 2, hk, dh), dtype) * 3
+    v = draw(gen, (n + 2, hk, dh), dtype)
+    k[0, 0] = 0  # a row of zeros
+    sections = (dh // 2 - 10, 10)
+    rot = Rotary(dh, sections)
+    pos = torch.randint(0, 5000, (2, n + 2), generator=gen)
+    cache = PagedCache.zeros(n_pages, ps, hk, dh, CODE[store])
+    for t in (cache.k, cache.v):
+        t.view(torch.uint8).fill_(7)
+    b = batch(cu, lens, table)
+    cache.write(b, k.to(DEV), v.to(DEV), rotary=rot, positions=pos.to(DEV))
+
+    rk = ref.rotate(f64(k), ref.rotary_angles(pos.numpy(), sections, 10000.0, "shared", dh // 2))
+    got = {m: getattr(cache, m).cpu() for m in ("k", "v")}
+    written = np.zeros((n_pages, ps), dtype=bool)
+    want_read = {m: np.zeros((n + 2, hk, dh)) for m in ("k", "v")}
+    for r, s, p in ref.rows_of(cu, lens):
+        at = ref.place(table[s], n_pages, ps, p)
+        if at is None:
+            continue
+        written[at] = True
+        for m, x in (("k", rk), ("v", f64(v))):
+            for h in range(hk):
+                stored = got[m][at[0], h, at[1]].float().double().numpy()
+                if store in ("fp8", "int8"):
+                    code, scale = ref.encode_row(x[r, h], store)
+                    np.testing.assert_array_equal(stored, code)
+                    assert getattr(cache, m + "_scale").cpu()[at[0], h, at[1]].item() == scale
+                    want_read[m][r, h] = code * scale
+                else:
+                    both = 2 * np.abs(f64(k)[r, h]).max()
+                    tol = ROUND[dtype] * np.abs(x[r, h]) + (8 * 2.0 ** -24 * both if m == "k" else 0)
+                    assert np.all(np.abs(stored - x[r, h]) <= tol)
+                    want_read[m][r, h] = stored
+    # nothing else was touched
+    for m in ("k", "v"):
+        raw = got[m].view(torch.uint8).numpy().reshape(n_pages, hk, ps, -1)
+        assert np.all(raw.transpose(0, 2, 1, 3)[~written] == 7)
+
+    out = [torch.full((n + 2, hk, dh), 77.0, dtype=DT[dtype], device=DEV) for _ in range(2)]
+    cache.read(b, n + 2, out=(out[0], out[1]))
+    for m, o in zip(("k", "v"), out):
+        back = f64(o)
+        assert np.all(back[n:] == 77)  # rows of no sequence
+        exact = torch.from_numpy(want_read[m]).float().to(DT[dtype])  # code * scale in fp32, rounded once
+        assert np.array_equal(back[:n], f64(exact)[:n])
+
+
+@pytest.mark.parametrize("store", ["fp8", "int8"])
+def test_quantiser_borders(store):
+    """Values on and next to the borders between codes, powers of two, subnormal rows and every code itself."""
+    gen = torch.Generator().manual_seed(11)
+    dh, rows = 64, []
+    grid = ref.E4M3 if store == "fp8" else np.arange(128.0)
+    mids = (grid[1:] + grid[:-1]) / 2
+    for scale in (1.0, 2.0 ** -20, 2.0 ** 30, 2.0 ** -126, 0.37, 1.0000001):
+        vals = np.concatenate([grid, mids, np.nextafter(np.float32(mids), np.float32(0)), np.nextafter(np.float32(mids), np.float32(1e9))])
+        vals = np.float32(vals) * np.float32(scale)
+        top = np.float32(grid[-1]) * np.float32(scale)
+        for at in range(0, len(vals), dh - 1):
+            part = vals[at:at + dh - 1]
+            rows.append(np.concatenate([[top], part, np.zeros(dh - 1 - len(part))]).astype(np.float32))
+    for e in (-149, -140, -130, -127, -126, 0, 100, 126):
+        rows.append((np.random.RandomState(e + 200).uniform(-1, 1, dh) * 2.0 ** e).astype(np.float32))
+        rows.append(np.full(dh, np.float32(1.75 * 2.0 ** e if e > -126 else 2.0 ** e)))
+    x = torch.from_numpy(np.stack(rows))[:, None].clone()
+    x *= torch.where(torch.rand(x.shape, generator=gen) < 0.5, -1.0, 1.0)
+    n = x.shape[0]
+    cache = PagedCache.zeros(-(-n // 64), 64, 1, dh, CODE[store])
+    b = batch(torch.tensor([0, n], dtype=torch.int32), torch.tensor([n], dtype=torch.int32),
+              torch.arange(-(-n // 64), dtype=torch.int32)[None])
+    cache.write(b, x.to(DEV), x.to(DEV))
+    code = cache.v.cpu().float().reshape(-1, dh)[:n].double().numpy()
+    scale = cache.v_scale.cpu().reshape(-1)[:n].double().numpy()
+    for r in range(n):
+        want, s = ref.encode_row(f64(x)[r, 0], store)
+        assert scale[r] == s
+        np.testing.assert_array_equal(code[r], want)
+    assert torch.equal(cache.k.view(torch.uint8), cache.v.view(torch.uint8))
+
+
+@pytest.mark.parametrize("store", ["fp8", "int8"])
+def test_rows_that_are_not_finite_read_as_nan(store):
+    dh = 128
+    x = torch.randn(4, 2, dh, generator=torch.Generator().manual_seed(3))
+    x[0, 1, 5], x[2, 0, 127], x[3, 1, 64] = float("nan"), float("inf"), -float("inf")
+    cache = PagedCache.zeros(1, 4, 2, dh, CODE[store])
+    b = batch(*[torch.tensor(t, dtype=torch.int32) for t in ([0, 4], [4], [[0]])])
+    cache.write(b, x.to(DEV), x.to(DEV), rotary=Rotary(dh))
+    k, v = cache.read(b, 4, dtype=torch.float32)
+    bad = torch.zeros(4, 2, dtype=torch.bool)
+    bad[0, 1] = bad[2, 0] = bad[3, 1] = True
+    for t in (k, v):
+        assert torch.equal(t.isnan().all(-1).cpu(), bad) and torch.equal(t.isnan().any(-1).cpu(), bad)
+
+
+def test_default_positions_are_the_tokens_indices():
+    gen = torch.Generator().manual_seed(8)
+    cu, lens, table, n_pages = pool([3, 5], [10, 900], 16, gen)
+    k = draw(gen, (8, 2, 64), "f32").to(DEV)
+    rot, b = Rotary(64, (16, 16)), batch(cu, lens, table)
+    one, two = (PagedCache.zeros(n_pages, 16, 2, 64, torch.float32) for _ in range(2))
+    one.write(b, k, k, rotary=rot)
+    two.write(b, k, k, rotary=rot, positions=torch.tensor([7, 8, 9, 895, 896, 897, 898, 899], device=DEV))
+    assert torch.equal(one.k, two.k) and torch.equal(one.v, two.v) and bool(one.k.any())
+
+
+# ---------------------------------------------------------------------------
+# attention
+# ---------------------------------------------------------------------------
+def check_attention(q, cache, kv, cu, lens, table, causal, window, dtype, max_length=0, b=None, out=None):
+    dh = q.shape[-1]
+    scale = dh ** -0.5
+    got = f64(cache.attend(b or batch(cu, lens, table, max_length), q.to(DEV), causal=causal, window=window, out=out))
+    want, spread, reach = ref.attend(f64(q), *kv, cu.numpy(), lens.numpy(), table.numpy(), causal, window, scale)
+    rows = ~np.isnan(want[:, 0, 0])
+    moved = 2 * (2 * (dh + 4) * 2.0 ** -24 * reach + 2.0 ** -21 + 64 * 2.0 ** -24) + (2.0 ** -8 if dtype == "bf16" else 0)
+    # what lies under the smallest normal number (2^-126) may be taken as 0: a probability, which then misses that
+    # share of its |v|, and the result
+    under = 2.0 ** -126 * (1 + max(int(lens.max()), 0) * np.abs(kv[1]).max())
+    tol = moved * spread + ROUND[dtype] * np.abs(want) + under
+    off = np.abs(got - want)[rows] - tol[rows]
+    assert not np.isnan(off).any()
+    assert off.max(initial=-1) <= 0, (off.max(), np.argwhere(off > 0)[:5])
+    return got
+
+
+ATTEND = {
+    # (new, length) of each sequence, query heads, kv heads, head dim, page size, causal, window
+    "one_token": ([(1, 1)], 8, 1, 256, 16, True, 0),
+    "tokens_ragged": ([(1, 817), (1, 1), (1, 64), (1, 65), (1, 0), (1, 300)], 8, 1, 256, 16, True, 0),
+    "tokens_mha": ([(1, 129), (1, 31)], 3, 3, 64, 32, True, 0),
+    "tokens_gqa5": ([(1, 500)] * 3, 10, 2, 128, 64, True, 0),
+    "wide_group": ([(1, 70), (2, 40)], 40, 1, 64, 8, True, 0),
+    "page_of_one": ([(5, 90)], 2, 1, 128, 1, True, 0),
+    "chunk": ([(51, 400)], 8, 1, 256, 64, False, 0),
+    "chunk_causal": ([(130, 259), (33, 33)], 4, 2, 128, 16, True, 0),
+    "prefill": ([(300, 300)], 2, 1, 64, 128, True, 0),
+    "window": ([(100, 300), (1, 300), (40, 40)], 4, 2, 64, 16, True, 37),
+    "window_of_one": ([(20, 33)], 2, 2, 128, 8, True, 1),
+    "window_full": ([(20, 200)], 4, 1, 128, 32, False, 50),
+    "rows_without_keys": ([(9, 4), (3, 0), (0, 7), (2, 5)], 6, 2, 64, 4, True, 0),
+    "mixed": ([(1, 650), (70, 210), (0, 9), (1, 3), (200, 330), (17, 1000)], 4, 1, 128, 64, True, 0),
+    "large_page": ([(3, 1500)], 2, 1, 256, 1024, True, 0),
+}
+
+
+@pytest.mark.parametrize("dtype,store", [("bf16", "bf16"), ("bf16", "fp8"), ("bf16", "int8"), ("f32", "f32"),
+                                         ("f32", "fp8"), ("f32", "int8")])
+@pytest.mark.parametrize("case", sorted(ATTEND))
+def test_attention(case, dtype, store):
+    seqs, hq, hk, dh, ps, causal, window = ATTEND[case]
+    gen = torch.Generator().manual_seed(sum(map(ord, case)))
+    cu, lens, table, n_pages = pool([s[0] for s in seqs], [s[1] for s in seqs], ps, gen)
+    cache, k, v = filled(n_pages, hk, ps, dh, store, gen)
+    q = draw(gen, (int(cu[-1]), hq, dh), dtype)
+    check_attention(q, cache, (k, v), cu, lens, table, causal, window, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [64, 128, 256])
+def test_attention_strided_rows_and_rows_of_no_sequence(dtype, dh):
+    """Queries as a slice of packed projections, the result into a slice; rows before the first and behind the last
+    sequence stay as they were."""
+    gen = torch.Generator().manual_seed(dh)
+    hq, hk, ps = 4, 2, 16
+    cu, lens, table, n_pages = pool([3, 40], [100, 61], ps, gen)
+    cu = cu + 2
+    n = int(cu[-1]) + 3
+    cache, k, v = filled(n_pages, hk, ps, dh, dtype, gen)
+    packed = draw(gen, (n, hq + 2 * hk, dh), dtype)
+    q = packed.to(DEV)[:, 1:1 + hq]
+    wide = torch.full((n, 2 * hq, dh), 77.0, dtype=DT[dtype], device=DEV)
+    out = wide[:, hq:]
+    check_attention(q, cache, (k, v), cu, lens, table, True, 0, dtype, out=out)
+    assert bool((wide[:, :hq] == 77).all() and (wide[:2] == 77).all() and (wide[n - 3:] == 77).all())
+
+
+@pytest.mark.parametrize("dtype,store", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32"), ("f32", "int8")])
+@pytest.mark.parametrize("new", [1, 40])
+def test_absent_pages_are_not_seen(dtype, store, new):
+    """Table entries outside the pool, and tokens beyond the table."""
+    gen = torch.Generator().manual_seed(4)
+    ps, dh = 16, 128
+    cu, lens, table, n_pages = pool([new, new], [400, 300], ps, gen)
+    table[0, 3], table[0, 7:10], table[1, 0], table[1, 5] = -1, n_pages, 2 ** 31 - 1, -2 ** 31
+    lens[1] = 40 * ps  # the table holds 25 pages
+    cache, k, v = filled(n_pages, 2, ps, dh, store, gen)
+    q = draw(gen, (2 * new, 4, dh), dtype)
+    check_attention(q, cache, (k, v), cu, lens, table, True, 0, dtype)
+    table[:] = -1
+    got = cache.attend(batch(cu, lens, table), q.to(DEV))
+    assert not bool(got.any())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [64, 256])
+@pytest.mark.parametrize("new,length,window", [(1, 40, 0), (70, 170, 0), (200, 700, 64), (16, 4000, 1000)])
+def test_what_is_not_seen_does_not_matter(dtype, dh, new, length, window):
+    """NaN and infinities in every slot that no row sees, and in the last tokens' K/V, which only they see."""
+    gen = torch.Generator().manual_seed(9)
+    ps, hk = 32, 1
+    cu, lens, table, n_pages = pool([new], [length], ps, gen)
+    cache, k, v = filled(n_pages, hk, ps, dh, dtype, gen)
+    seen = np.zeros((n_pages, ps), dtype=bool)
+    first = max(0, length - new - window + 1) if window else 0
+    for j in range(first, length):
+        seen[ref.place(table[0], n_pages, ps, j)] = True
+    hide = torch.from_numpy(~seen)
+    q = draw(gen, (new, 2, dh), dtype)
+    for junk in (float("nan"), float("inf")):
+        for t in (cache.k, cache.v):
+            t.permute(0, 2, 1, 3)[hide.to(DEV)] = junk
+        check_attention(q, cache, (k, v), cu, lens, table, True, window, dtype)
+    if new > 1:
+        at = ref.place(table[0], n_pages, ps, length - 1)
+        cache.v[at[0], :, at[1], 3] = float("inf")
+        cache.v[at[0], :, at[1], 4] = float("nan")
+        got = cache.attend(batch(cu, lens, table), q.to(DEV), window=window)
+        want = check_attention(q[:-1], cache, (k, v), cu - torch.tensor([0, 1], dtype=torch.int32),
+                               lens - 1, table, True, window, dtype)
+        assert bool(got[:-1].isfinite().all())
+        np.testing.assert_allclose(f64(got[:-1]), want, atol=0.05 if dtype == "bf16" else 1e-4)
+        assert bool(torch.isposinf(got[-1, :, 3]).all() and got[-1, :, 4].isnan().all() and got[-1, :, 5:].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype,store", [("bf16", "bf16"), ("bf16", "int8"), ("f32", "f32")])
+def test_large_scores_and_queries_that_are_not_finite(dtype, store):
+    """Scores far apart (one key takes all) and running maxima that move; a NaN query keeps to its row."""
+    gen = torch.Generator().manual_seed(21)
+    cu, lens, table, n_pages = pool([50], [900], 16, gen)
+    cache, k, v = filled(n_pages, 1, 16, 128, store, gen)
+    q = draw(gen, (50, 4, 128), dtype) * torch.exp(torch.linspace(-3, 4, 50))[:, None, None].to(DT[dtype])
+    check_attention(q, cache, (k, v), cu, lens, table, True, 0, dtype)
+    clean = cache.attend(batch(cu, lens, table), q.to(DEV))
+    q[17, 2, 5] = float("nan")
+    got = cache.attend(batch(cu, lens, table), q.to(DEV))
+    assert bool(got[17, 2].isnan().all())
+    got[17, 2] = clean[17, 2]
+    assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("dtype,store", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32")])
+@pytest.mark.parametrize("new", [1, 3, 100])
+def test_max_length_only_sizes_the_launch(dtype, store, new):
+    """A hint that is too short, and results that are the same bit for bit from call to call."""
+    gen = torch.Generator().manual_seed(2)
+    cu, lens, table, n_pages = pool([new, new], [5000, 70 + new], 64, gen, more_pages=3)
+    cache, k, v = filled(n_pages, 1, 64, 128, store, gen)
+    q = draw(gen, (2 * new, 8, 128), dtype)
+    for hint in (0, 64, 100000):
+        check_attention(q, cache, (k, v), cu, lens, table, True, 0, dtype, max_length=hint)
+    b = batch(cu, lens, table)
+    assert torch.equal(cache.attend(b, q.to(DEV)), cache.attend(b, q.to(DEV)))
+
+
+def test_scale_of_zero_and_sharing_pages():
+    """scale 0 gives the mean of the visible values; sequences that share their prefix's pages."""
+    gen = torch.Generator().manual_seed(6)
+    cu, lens, table, n_pages = pool([2, 1, 3], [40, 40, 37], 8, gen)
+    table[1, :4] = table[0, :4]
+    table[2, :2] = table[0, :2]
+    cache, k, v = filled(n_pages, 1, 8, 64, "f32", gen)
+    q = draw(gen, (6, 2, 64), "f32")
+    check_attention(q, cache, (k, v), cu, lens, table, True, 0, "f32")
+    got = f64(cache.attend(batch(cu, lens, table), q.to(DEV), causal=False, scale=0.0))
+    mean = np.mean([v[p // 1][0, s] for p, s in (ref.place(table[0], n_pages, 8, j) for j in range(40))], 0)
+    np.testing.assert_allclose(got[0, 0], mean, atol=1e-5)
+
+
+def test_offsets_past_32_bits():
+    """A pool whose pages begin past 2^32 bytes of codes, written, read and attended at its end."""
+    dh, ps, hk = 256, 1024, 8
+    n_pages = 2 ** 32 // (dh * ps * hk) + 2
+    gen = torch.Generator().manual_seed(1)
+    cache = PagedCache.zeros(n_pages, ps, hk, dh, torch.int8)
+    n = 40
+    table = torch.tensor([[n_pages - 1, 0]], dtype=torch.int32)
+    cu, lens = torch.tensor([0, n], dtype=torch.int32), torch.tensor([n], dtype=torch.int32)
+    b = batch(cu, lens, table)
+    k, v = draw(gen, (n, hk, dh), "bf16"), draw(gen, (n, hk, dh), "bf16")
+    cache.write(b, k.to(DEV), v.to(DEV))
+    assert not bool(cache.k[:-1].any())
+    rk, rv = cache.read(b, n)
+    for x, y in ((k, rk), (v, rv)):
+        assert float((y.cpu().float() - x.float()).abs().max()) <= float(x.float().abs().max()) * (0.5 / 127 + 2.0 ** -8)
+    q = draw(gen, (n, hk, dh), "bf16")
+    kv = [f64(t.cpu()).transpose(1, 0, 2)[None] for t in cache.read(b, n, dtype=torch.float32)]
+    small = (torch.zeros(1, 1, dtype=torch.int32), )
+    want, spread, reach = ref.attend(f64(q), *kv, cu.numpy(), lens.numpy(), small[0].numpy(), True, 0, dh ** -0.5)
+    got = f64(cache.attend(b, q.to(DEV)))
+    assert np.all(np.abs(got - want) <= 2.0 ** -7 * spread + 2.0 ** -8 * np.abs(want))
+
+
+# ---------------------------------------------------------------------------
+# streams, graphs, the engine
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("new", [1, 24])
+def test_captured_graph_follows_the_lengths(new):
+    """Write and attend captured once, replayed while the sequences grow in device memory; two graphs captured one
+    after the other and replayed in turn; every replay against the eager result."""
+    gen = torch.Generator().manual_seed(13)
+    ps, dh, hk, hq = 16, 128, 2, 8
+    cu, lens, table, n_pages = pool([new, new], [2000, 1500], ps, gen)
+    b = batch(cu, lens.clone(), table, 2000)
+    cache = PagedCache.zeros(n_pages, ps, hk, dh, torch.float8_e4m3fn)
+    rot = Rotary(dh)
+    k, v, q = (draw(gen, (2 * new, h, dh), "bf16").to(DEV) for h in (hk, hk, hq))
+    dlens = b.tensors[1]
+
+    def step():
+        cache.write(b, k, v, rotary=rot)
+        return cache.attend(b, q)
+
+    dlens.copy_(torch.tensor([new, new], dtype=torch.int32))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graphs, outs = [], []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(step())
+        graphs.append(g)
+    for i, n in enumerate((new, 100, 777, 1500)):
+        dlens.fill_(n)
+        k.copy_(draw(gen, k.shape, "bf16"))
+        q.copy_(draw(gen, q.shape, "bf16"))
+        graphs[i % 2].replay()
+        got = outs[i % 2].clone()
+        torch.cuda.synchronize()
+        assert torch.equal(got, step())
+
+
+def test_streams():
+    """Two calls at once on two streams, each with its own workspace, against the calls one by one."""
+    gen = torch.Generator().manual_seed(17)
+    cu, lens, table, n_pages = pool([1] * 4, [3000] * 4, 64, gen)
+    cache, _, _ = filled(n_pages, 1, 64, 256, "bf16", gen)
+    b = batch(cu, lens, table)
+    qs = [draw(gen, (4, 8, 256), "bf16").to(DEV) for _ in range(2)]
+    want = [cache.attend(b, q) for q in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(cache.attend(b, qs[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(g, want[i]) for g in got[i])
+
+
+def test_python_refusals_on_the_gpu():
+    gen = torch.Generator().manual_seed(1)
+    cu, lens, table, n_pages = pool([2], [20], 16, gen)
+    cache, b = PagedCache.zeros(n_pages, 16, 2, 64), batch(cu, lens, table)
+    ok = torch.zeros(2, 2, 64, dtype=torch.bfloat16, device=DEV)
+    for bad in (ok.cpu(), ok[:, :1], ok.half(), ok.clone().requires_grad_(), ok.transpose(1, 2).contiguous().transpose(1, 2)):
+        with pytest.raises(ValueError):
+            cache.write(b, bad, bad)
+    with pytest.raises(R.ReflexError):
+        cache.write(b, ok.float(), ok.float())  # bf16 pages
+    with pytest.raises(R.ReflexError):
+        cache.attend(b, torch.zeros(2, 3, 64, dtype=torch.bfloat16, device=DEV))  # 3 heads on 2
+    odd = torch.zeros(2 * 2 * 64 + 1, dtype=torch.bfloat16, device=DEV)[1:].view(2, 2, 64)
+    with pytest.raises(R.ReflexError):
+        cache.attend(b, odd)  # not on a 16-byte boundary
+    with pytest.raises(ValueError):
+        cache.write(b, ok, ok, positions=torch.zeros(2, dtype=torch.int64, device=DEV))
+    with pytest.raises(ValueError):
+        cache.write(b, ok, ok, rotary=Rotary(64), positions=torch.zeros(3, dtype=torch.int64, device=DEV))
+    with pytest.raises(ValueError):
+        cache.write(b, ok, ok, rotary=Rotary(64), positions=torch.zeros(2, dtype=torch.int32, device=DEV))
