@@ -118,6 +118,21 @@ def test_null_structs():
     assert lib.reflex_rotary_apply(b(plan()), None, 0, b(r), b(r), 1, 1, 1, 0, None) == R.REFLEX_EINVAL
 
 
+def test_workspace_is_required_and_checked():
+    """A single row over a long memory splits its keys: the call names its bytes and refuses less."""
+    lib, b = R.load_library(), ctypes.byref
+    c, q = cache_c(n_pages=4096), batch_c(max_pages=1024, n_seqs=1)
+    need = ctypes.c_size_t(0)
+    assert lib.reflex_paged_attention_workspace(b(c), b(q), 1, 4, R.DTYPE_BF16, b(need)) == R.REFLEX_OK
+    assert need.value > 0
+    for ws, nb in ((None, need.value), (A, need.value - 1), (A + 16, need.value)):
+        assert attend(cache=c, batch=q, n=1, ws=ws, nb=nb) == R.REFLEX_EINVAL
+    # a longer memory never needs less, and a huge batch needs no more than its rows' partials
+    more = ctypes.c_size_t(0)
+    assert lib.reflex_paged_attention_workspace(b(c), b(q), 4096, 4, R.DTYPE_BF16, b(more)) == R.REFLEX_OK
+    assert more.value <= 4096 * 4 * 64 * (64 + 2) * 4
+
+
 @pytest.mark.parametrize("args", [
     (60, (30,)), (0, (0,)), (272, (136,)), (64, (31,)), (64, (33,)), (64, (-1, 33)), (64, ()), (64, (8, 8, 8, 4, 4))])
 def test_bad_rotary_plans(args):
