@@ -1,5 +1,6 @@
 // Attention of a chunk of new tokens over a paged cache.
 #include <algorithm>
+#include <type_traits>
 
 #include "paged.h"
 
@@ -10,6 +11,9 @@ namespace {
 // Running maxima start here instead of at -infinity, so that a row that sees
 // nothing has exp2(-infinity - m) = 0 and not NaN.
 constexpr float kFloor = -3.0e38f;
+
+// what a copy into LDS reads in place of a row that is not there
+__device__ const uint4 kZeros[1] = {};
 
 // Keys that a query at token `pos` of a sequence of `len` sees: [lo, hi).
 struct Span { int lo, hi; };
@@ -356,24 +360,26 @@ __global__ __launch_bounds__(256) void paged_attn_few_kernel(const PagedAttnArgs
     __syncthreads();
     const int n_t = (seg_end - seg + KT - 1) / KT;
 
-    // this lane's key of tile `x`: its page row, or -1
+    // this lane's key of tile `x`: its page row, or -1 where no row of the tile
+    // sees it: such values must not meet a probability of 0
+    const int v_lo = max(k_beg, lo_min), v_hi = min(hi_max, seg_end);
     auto row_of = [&](int x) __attribute__((always_inline)) {
       const int key = seg + x * KT + lane;
-      if (lane >= KT || key >= seg_end) return -1;
+      if (lane >= KT || key < v_lo || key >= v_hi) return -1;
       const int pg = table[(key >> shift) - e0];
       return pg < 0 ? -1 : ((pg * n_kv) << shift) + (key & ((1 << shift) - 1));
     };
-    // copy a tile's K or V; r: this lane's page row (or -1: any row will do)
+    // copy a tile's K or V; r: this lane's page row; zeros where it has none
     auto copy = [&](const char* base, const float* sc, int r, unsigned char* dst, float* sdst)
         __attribute__((always_inline)) {
-      const int64_t rr = (int64_t)max(r, 0) + hoff;
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
         const int row = (j * 64 + lane) / NCH, ch = (lane + j * 64) % NCH;
-        const int pr = __shfl(max(r, 0), row, 64);
-        lds_dma16(base + ((int64_t)pr + hoff) * RB + ((ch ^ swz(row)) << 4), dst + j * 1024);
+        const int pr = __shfl(r, row, 64);
+        const char* src = base + ((int64_t)pr + hoff) * RB + ((ch ^ swz(row)) << 4);
+        lds_dma16(pr < 0 ? reinterpret_cast<const char*>(kZeros) : src, dst + j * 1024);
       }
-      if (Q8) lds_dma4(sc + rr, sdst);
+      if (Q8) lds_dma4(sc + (int64_t)max(r, 0) + hoff, sdst);
     };
     constexpr int NC = NI + (Q8 ? 1 : 0);
 
@@ -473,15 +479,6 @@ __global__ __launch_bounds__(256) void paged_attn_few_kernel(const PagedAttnArgs
       }
 
       wait_copies_if<NC>(more);
-      if (!whole) {
-        // values that no row of the tile sees must not meet a probability of 0
-        const int v_lo = max(k_beg, lo_min), v_hi = min(hi_max, seg_end);
-#pragma unroll
-        for (int j = 0; j < NI; ++j) {
-          const int at = (j * 64 + lane) / NCH, key = key0 + at;
-          if (key < v_lo || key >= v_hi || !((present >> at) & 1)) st16(vb + j * 1024 + lane * 16, zero16());
-        }
-      }
       if (Q8) {
 #pragma unroll
         for (int b = 0; b < NKB; ++b) {
@@ -590,6 +587,358 @@ __global__ __launch_bounds__(256) void paged_attn_few_kernel(const PagedAttnArgs
   }
 }
 
+// ---------------------------------------------------------------------------
+// many rows (bf16): one workgroup per 128 rows, K/V head and key split
+// ---------------------------------------------------------------------------
+// Bound by the matrix products.  Four waves hold 32 query rows each and share
+// tiles of 64 keys, copied straight from the pages into two buffers of LDS.
+// As in the few-row kernel scores are formed transposed and V is read through
+// transposing LDS reads, so that probabilities stay in registers; here with
+// the 32x32x16 product.  A wave forms the scores of tile t + 1 while it takes
+// the softmax of tile t, so that its vector work runs under its matrix work;
+// K of tile t + 2 and V of tile t + 1 are on their way meanwhile, with one
+// barrier a tile.  The running maximum of a row is raised only when a score
+// exceeds it by 2^8 (kSlack): probabilities then stay below 2^8 and the
+// output's accumulators are rescaled in few tiles.
+constexpr float kSlack = 8.f;
+
+template <int ST, int DH>
+struct ManyCfg {
+  static constexpr bool Q8 = ST == REFLEX_STORE_FP8 || ST == REFLEX_STORE_INT8;
+  static constexpr int ES = Q8 ? 1 : 2;
+  static constexpr int RB = DH * ES;
+  static constexpr int KT = 64;
+  static constexpr int NCH = RB / 16;
+  static constexpr int RPC = 64 / NCH;           // rows of a copy
+  static constexpr int TB = KT * RB;
+  static constexpr int NI = TB / 1024 / 4;       // copies of a wave and tile (K or V)
+  static constexpr int XB = 128 * (DH + 4) * 4;  // the exchange at the end
+  static constexpr int SMEM = 4 * TB > XB ? 4 * TB : XB;
+  static constexpr int kTable = 1024;
+};
+
+template <int ST, int DH>
+__global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel(const PagedAttnArgs a, int tiles) {
+  typedef ManyCfg<ST, DH> C;
+  typedef bf16_t T;
+  constexpr bool Q8 = C::Q8;
+  constexpr int KT = C::KT, RB = C::RB, NCH = C::NCH, NI = C::NI, RPC = C::RPC, TB = C::TB;
+  constexpr int NKS = DH / 16, NDB = DH / 32, BM = 128, OP = DH + 4;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[C::SMEM];
+  __shared__ float scales[2][2][KT];
+  __shared__ int table[C::kTable];
+  __shared__ float2 ml[BM];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r32 = lane & 31, h = lane >> 5;
+  // consecutive workgroups go to the eight XCDs in turn: each XCD takes a run
+  // of (head, split) groups, so that a group's tiles share its L2, and a
+  // group's last tiles (with a causal mask the longest) first
+  const int per = gridDim.x >> 3;
+  const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  const int grp = id / tiles;
+  if (grp >= a.c.n_kv * a.nsplit) return;
+  const int kvh = grp / a.nsplit, split = grp - kvh * a.nsplit;
+  Tile t;
+  if (!find_tile(a, tiles - 1 - (id - grp * tiles), BM, lane, t)) return;
+
+  const int rows_here = min(BM, t.rows - t.r0);
+  const int p0 = t.first_pos + t.r0 / a.group, p1 = t.first_pos + (t.r0 + rows_here - 1) / a.group;
+  const Span sp0 = span_of(a, p0, t.len), sp1 = span_of(a, p1, t.len);
+  const int s_beg = split * a.split_keys;
+  const int s_end = split == a.nsplit - 1 ? INT32_MAX : s_beg + a.split_keys;
+  const int k_beg = max(sp0.lo, s_beg), k_end = min(sp1.hi, s_end);
+
+  const int r = t.r0 + 32 * wave + r32;
+  const int tok = r / a.group;
+  const Span sp = span_of(a, t.first_pos + tok, t.len);
+  const int lo = max(sp.lo, s_beg), hi = r < t.rows ? min(sp.hi, s_end) : 0;
+  // the keys that all of the wave's rows see
+  const int w0 = min(t.r0 + 32 * wave, t.rows - 1), w1 = min(w0 + 31, t.rows - 1);
+  const int all_lo = max(span_of(a, t.first_pos + w1 / a.group, t.len).lo, s_beg);
+  const int all_hi = min(span_of(a, t.first_pos + w0 / a.group, t.len).hi, s_end);
+  uint4 qf[NKS];
+  {
+    const T* qp = reinterpret_cast<const T*>(a.x.p) + (t.first_row + tok) * a.x.rs +
+                  (int64_t)(kvh * a.group + (r - tok * a.group)) * a.x.hs;
+#pragma unroll
+    for (int k = 0; k < NKS; ++k) {
+      const int d = Q8 ? 32 * (k >> 1) + 16 * h + 8 * (k & 1) : 16 * k + 8 * h;
+      qf[k] = r < t.rows ? ld16(qp + d) : zero16();
+    }
+  }
+  f32x16_v o[NDB];
+#pragma unroll
+  for (int d = 0; d < NDB; ++d) o[d] = f32x16_v{};
+  float mx = kFloor, sum = 0.f;
+
+  const int64_t hoff = (int64_t)kvh << a.c.shift;
+  const int shift = a.c.shift, n_pages = a.c.n_pages, n_kv = a.c.n_kv;
+  const char *const pk = a.c.k, *const pv = a.c.v;
+  const float *const psk = a.c.k_scale, *const psv = a.c.v_scale;
+  const float scale2 = a.scale2;
+  const bool in_page = (1 << shift) >= RPC;  // the rows of a copy lie in one page
+  // Swizzles of the 16-byte chunks of a row in LDS: K reads take one chunk of
+  // 32 rows at a time, V reads 64 bytes of 8 rows.  They are XORs, and rows
+  // are powers of two apart, so the address of every read is one of few
+  // registers plus a constant.
+  auto swk = [](int row) __attribute__((always_inline)) { return row & (NCH - 1) & 15; };
+  auto swv = [](int row) __attribute__((always_inline)) { return (Q8 ? row : 2 * row) & (NCH - 1); };
+  constexpr int NKR = NCH / 2 < 8 ? NCH / 2 : 8;   // K reads: chunk pairs 2 k, by their low four bits
+  constexpr int NVR = Q8 ? NDB : NDB < 4 ? NDB : 4;  // V reads: blocks d, in bf16 by their low two bits
+  uint32_t kreg[NKR], vreg[NVR];
+#pragma unroll
+  for (int k = 0; k < NKR; ++k) kreg[k] = r32 * RB + (((2 * k + h) ^ swk(r32)) << 4);
+  {
+    const int i16 = lane & 15, dh16 = (lane >> 4) & 1, r8 = i16 >> 1;
+    const int row = 4 * h + (Q8 ? (r8 < 4 ? r8 : r8 + 4) : i16 >> 2);
+#pragma unroll
+    for (int d = 0; d < NVR; ++d) {
+      const int ch = Q8 ? 2 * d + dh16 : 4 * d + 2 * dh16 + ((i16 >> 1) & 1);
+      vreg[d] = 2 * TB + row * RB + ((ch ^ swv(row)) << 4) + (i16 & 1) * 8;
+    }
+  }
+  // this lane's offset within its wave's first copy of a tile; the swizzle of
+  // the others differs by a constant
+  const int sub = lane / NCH;
+  const uint32_t koff = sub * RB + (((lane % NCH) ^ swk(sub)) << 4);
+  const uint32_t voff = sub * RB + (((lane % NCH) ^ swv(sub)) << 4);
+
+  for (int seg = k_beg & ~(KT - 1); seg < k_end;) {
+    const int e0 = seg >> shift;
+    const int seg_end = (int)min((int64_t)k_end, (int64_t)(e0 + C::kTable) << shift);
+    const int ne = ((seg_end - 1) >> shift) - e0 + 1;
+    __syncthreads();
+    int good = 1;
+    for (int i = threadIdx.x; i < ne; i += 256) {
+      const int pg = a.q.table[(int64_t)t.b * a.q.max_pages + e0 + i];
+      const bool ok = (unsigned)pg < (unsigned)n_pages;
+      table[i] = ok ? pg : -1;
+      good &= ok;
+    }
+    const bool seg_ok = __syncthreads_and(good);
+    const int n_t = (seg_end - seg + KT - 1) / KT;
+
+    auto row_of = [&](int x) __attribute__((always_inline)) {
+      const int key = seg + x * KT + lane;
+      const int pg = table[(min(key, seg_end - 1) >> shift) - e0];
+      return key < k_beg || key >= seg_end || pg < 0 ? -1 : ((pg * n_kv) << shift) + (key & ((1 << shift) - 1));
+    };
+    // rr: the lane's page row.  Mostly all 64 are there and a copy's rows lie in
+    // one page: then only a uniform base and the lane's offset are needed.
+    auto copy = [&](const char* base, auto sw, uint32_t off, int rr, unsigned char* dst) __attribute__((always_inline)) {
+      if (in_page && !__ballot(rr < 0)) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          const int pr = __builtin_amdgcn_readlane(rr, (wave * NI + j) * RPC);
+          lds_dma16(base + ((int64_t)pr + hoff) * RB, off ^ (sw(j * RPC) << 4), dst + (wave * NI + j) * 1024);
+        }
+      } else {
+#pragma unroll 1
+        for (int j = 0; j < NI; ++j) {
+          const int pr = __shfl(rr, (wave * NI + j) * RPC + sub, 64);
+          const char* src = base + ((int64_t)pr + hoff) * RB + ((off ^ (sw(j * RPC) << 4)) - sub * RB);
+          lds_dma16(pr < 0 ? reinterpret_cast<const char*>(kZeros) : src, dst + (wave * NI + j) * 1024);
+        }
+      }
+    };
+    auto copy_k = [&](int x, int buf) __attribute__((always_inline)) {
+      const int rr = row_of(x);
+      copy(pk, swk, koff, rr, smem + buf * TB);
+    };
+    // (with the scales of the tile's keys: the softmax reads them while K of
+    // two tiles further is on its way)
+    auto copy_v = [&](int x, int buf) __attribute__((always_inline)) {
+      const int rr = row_of(x);
+      copy(pv, swv, voff, rr, smem + (2 + buf) * TB);
+      if (Q8 && wave < 2) lds_dma4((wave == 0 ? psk : psv) + max(rr, 0) + hoff, scales[wave][buf]);
+    };
+    // S^T of a tile: block b, register i holds key 32 b + 8 (i / 4) + 4 h + i % 4
+    auto scores = [&](uint32_t buf, f32x16_v (&s)[2]) __attribute__((always_inline)) {
+      s[0] = f32x16_v{};
+      s[1] = f32x16_v{};
+#pragma unroll
+      for (int k = 0; k < NCH / 2; ++k)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const uint4 c = ld16(smem + kreg[k % NKR] + buf + (k / NKR) * 256 + b * 32 * RB);
+          if (!Q8) {
+            mfma32_step(s[b], c, qf[k]);
+          } else {
+            mfma32_step(s[b], codes_to_bf16<ST>(make_uint2(c.x, c.y)), qf[2 * k]);
+            mfma32_step(s[b], codes_to_bf16<ST>(make_uint2(c.z, c.w)), qf[2 * k + 1]);
+          }
+        }
+    };
+    auto softmax = [&](int x, int buf, f32x16_v (&s)[2], uint4 (&pf)[4]) __attribute__((always_inline)) {
+      const int key0 = seg + x * KT;
+      const bool whole = seg_ok && key0 >= all_lo && key0 + KT <= all_hi && key0 + KT <= seg_end;
+      if (Q8) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float4 k4 = *reinterpret_cast<const float4*>(&scales[0][buf][32 * b + 8 * i + 4 * h]);
+            s[b][4 * i] *= k4.x; s[b][4 * i + 1] *= k4.y; s[b][4 * i + 2] *= k4.z; s[b][4 * i + 3] *= k4.w;
+          }
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[b][i] *= scale2;
+      if (!whole) {
+        const int l0 = lo - key0 - 4 * h, h0 = min(hi, seg_end) - key0 - 4 * h;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int at = 32 * b + 8 * (i >> 2) + (i & 3);
+            s[b][i] = at >= l0 && at < h0 ? s[b][i] : -INFINITY;
+          }
+        if (!seg_ok) {
+          const uint64_t present = __ballot(row_of(x) >= 0) >> (4 * h);
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (!((present >> (32 * b + 8 * (i >> 2) + (i & 3))) & 1)) s[b][i] = -INFINITY;
+        }
+      }
+      float top = kFloor;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+      {
+        auto z = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(z[0]), __uint_as_float(z[1]));
+      }
+      if (__ballot(top > mx + kSlack)) {
+        const float nm = top > mx + kSlack ? top : mx;
+        const float f = __builtin_amdgcn_exp2f(mx - nm);
+        mx = nm;
+        sum *= f;
+#pragma unroll
+        for (int d = 0; d < NDB; ++d) o[d] *= f;
+      }
+      float add = 0.f;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float p = __builtin_amdgcn_exp2f(s[b][i] - mx);
+          add += p;
+          s[b][i] = p;
+        }
+      sum += add;
+      if (Q8) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float4 v4 = *reinterpret_cast<const float4*>(&scales[1][buf][32 * b + 8 * i + 4 * h]);
+            const float vv[4] = {v4.x, v4.y, v4.z, v4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float p = s[b][4 * i + e];
+              // (a key that the row does not see may have any scale)
+              s[b][4 * i + e] = whole || p > 0.f || p != p ? p * vv[e] : 0.f;
+            }
+          }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const f32x16_v& v = s[u >> 1];
+        const int e = 8 * (u & 1);
+        pf[u] = make_uint4(pack_bf16(v[e], v[e + 1]), pack_bf16(v[e + 2], v[e + 3]), pack_bf16(v[e + 4], v[e + 5]),
+                           pack_bf16(v[e + 6], v[e + 7]));
+      }
+    };
+    // O^T += V^T P^T: step u covers keys 16 u + {4 h .., 8 + 4 h ..}
+    auto values = [&](uint32_t buf, const uint4 (&pf)[4]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int d = 0; d < NDB; ++d) {
+          uint4 f;
+          if (Q8) {
+            f = codes_to_bf16<ST>(ld_tr8(smem + vreg[d] + buf + 16 * u * RB));
+          } else {
+            // rows 8 further: the swizzle differs by 16 of the chunk's bits, if it has that many
+            const unsigned char* at = smem + vreg[d % NVR] + buf + 16 * u * RB;
+            constexpr int flip = NCH > 16 ? 1 : 0;
+            const uint2 f0 = ld_tr16(at + (d / NVR) * 256), f1 = ld_tr16(at + 8 * RB + ((d / NVR) ^ flip) * 256);
+            f = make_uint4(f0.x, f0.y, f1.x, f1.y);
+          }
+          mfma32_step(o[d], f, pf[u]);
+        }
+    };
+    // all of the wave's copies have landed and its reads are done, in every wave
+    auto turn = [&]() __attribute__((always_inline)) {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+
+    copy_k(0, 0);
+    copy_v(0, 0);
+    if (n_t > 1) copy_k(1, 1);
+    turn();
+    f32x16_v sa[2], sb[2];
+    scores(0, sa);
+    turn();
+    uint4 pf[4];
+    // one tile's softmax and values under the next one's scores and copies;
+    // B: the tile's buffers
+    auto step = [&](int x, auto B, f32x16_v (&cur)[2], f32x16_v (&nxt)[2]) __attribute__((always_inline)) {
+      constexpr int buf = decltype(B)::value;
+      if (x + 2 < n_t) copy_k(x + 2, buf);
+      copy_v(x + 1, buf ^ 1);
+      scores((buf ^ 1) * TB, nxt);
+      softmax(x, buf, cur, pf);
+      values(buf * TB, pf);
+      turn();
+    };
+    int x = 0;
+    for (; x + 2 < n_t; x += 2) {
+      step(x, std::integral_constant<int, 0>{}, sa, sb);
+      step(x + 1, std::integral_constant<int, 1>{}, sb, sa);
+    }
+    if (x + 1 < n_t) {
+      step(x, std::integral_constant<int, 0>{}, sa, sb);
+      ++x;
+      sa[0] = sb[0];
+      sa[1] = sb[1];
+    }
+    softmax(x, x & 1, sa, pf);
+    values((x & 1) * TB, pf);
+    seg = seg_end;
+  }
+
+  __syncthreads();
+  float* const ex = reinterpret_cast<float*>(smem) + wave * 32 * OP;
+  {
+    auto z = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+    if (h == 0) ml[32 * wave + r32] = make_float2(mx, __uint_as_float(z[0]) + __uint_as_float(z[1]));
+  }
+#pragma unroll
+  for (int d = 0; d < NDB; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<float4*>(ex + r32 * OP + 32 * d + 8 * i + 4 * h) =
+          make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
+  __syncthreads();
+  constexpr int N = DH / 64;
+  const bool mixed = sp0.lo != sp1.lo || sp0.hi != sp1.hi;
+  for (int q = 0; q < 32 && 32 * wave + q < rows_here; ++q) {
+    const int rq = t.r0 + 32 * wave + q, tq = rq / a.group;
+    const float2 w = ml[32 * wave + q];
+    float y[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = ex[q * OP + lane * N + i];
+    finish_row<T, ST, DH>(a, t, t.first_row + tq, kvh * a.group + (rq - tq * a.group), t.first_pos + tq, k_beg, k_end,
+                          split, mixed, w.x, w.y, y);
+  }
+}
+
 // One wave per (row, head): the splits' partial results joined.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void paged_attn_merge_kernel(const PagedAttnArgs a) {
@@ -636,19 +985,27 @@ int64_t tile_bound(int64_t n_rows, int n_seqs, int group, int bm) {
   return n_rows * group / bm + std::min<int64_t>(n_seqs, n_rows);
 }
 
-// 16-row blocks of a workgroup of the few-row kernel.
-int few_blocks(int64_t n_rows, int n_seqs, int group) {
-  return n_rows * group > 16 * (int64_t)std::max(1, n_seqs) ? 2 : 1;
+// Rows of a tile, by the rows of an average sequence: 16 or 32 with the few-row
+// kernel, 128 with the many-row one.
+int rows_of_tile(int64_t n_rows, int n_seqs, int group, int dtype) {
+  const int64_t rows = n_rows * group / std::max<int64_t>(1, std::min<int64_t>(n_seqs, n_rows));
+  return rows <= 16 ? 16 : rows <= 32 || dtype != REFLEX_DTYPE_BF16 ? 32 : 128;
 }
 
 template <typename T, int ST, int DH>
 hipError_t launch_shape(const PagedAttnArgs& a, hipStream_t s) {
-  const int mr = few_blocks(a.n_rows, a.q.n, a.group);
-  const int64_t tiles = tile_bound(a.n_rows, a.q.n, a.group, 16 * mr);
+  const int bm = rows_of_tile(a.n_rows, a.q.n, a.group, sizeof(T) == 2 ? REFLEX_DTYPE_BF16 : REFLEX_DTYPE_F32);
+  const int64_t tiles = tile_bound(a.n_rows, a.q.n, a.group, bm);
   const dim3 grid((unsigned)tiles, (unsigned)(a.c.n_kv * a.nsplit));
-  if (mr == 1)
+  if constexpr (sizeof(T) == 2) {
+    if (bm == 128) {
+      const unsigned n = (unsigned)((tiles * a.c.n_kv * a.nsplit + 7) / 8 * 8);
+      RFX_LAUNCH((paged_attn_many_kernel<ST, DH>), dim3(n), dim3(256), 0, s, a, (int)tiles);
+    }
+  }
+  if (bm == 16)
     RFX_LAUNCH((paged_attn_few_kernel<T, ST, DH, 1>), grid, dim3(256), 0, s, a);
-  else
+  else if (bm == 32)
     RFX_LAUNCH((paged_attn_few_kernel<T, ST, DH, 2>), grid, dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.nsplit > 1) {
@@ -673,10 +1030,12 @@ PagedAttnPlan paged_attention_plan(const reflex_paged_cache& c, const reflex_pag
   const int group = n_q / c.n_kv_heads;
   const int64_t cap = (int64_t)b.max_pages * c.page_size;
   const int64_t len = b.max_length > 0 && b.max_length < cap ? b.max_length : cap;
-  const int mr = few_blocks(n_rows, b.n_seqs, group);
-  const int64_t blocks = tile_bound(n_rows, b.n_seqs, group, 16 * mr) * c.n_kv_heads;
-  // enough workgroups for every CU four times over, each with 128 keys at least
-  int64_t want = (1024 + blocks - 1) / blocks;
+  const int bm = rows_of_tile(n_rows, b.n_seqs, group, dtype);
+  const int64_t blocks = tile_bound(n_rows, b.n_seqs, group, bm) * c.n_kv_heads;
+  // few rows: enough workgroups for every CU four times over, each with 128
+  // keys at least; many rows: at most one round of workgroups
+  const int64_t slots = c.head_dim > 128 && c.store < REFLEX_STORE_FP8 ? 256 : 512;
+  int64_t want = bm == 128 ? slots / blocks : (1024 + blocks - 1) / blocks;
   want = std::min<int64_t>(want, (len + 127) / 128);
   want = std::min<int64_t>(want, std::min<int64_t>(kMaxSplits, 65535 / c.n_kv_heads));
   want = std::max<int64_t>(want, 1);
