@@ -96,7 +96,8 @@ struct PagedAttnArgs {
   Rows x, o;         // queries, result
   int64_t n_rows;
   int n_q, group;    // query heads, query heads per K/V head
-  float scale2;      // scale * log2(e)
+  float scale2;      // |scale| * log2(e), at least the smallest normal number (a masked -inf stays -inf)
+  int negate;        // scale < 0: queries enter with the other sign
   int causal, window;
   int nsplit;        // key splits; with more than one, partials go to the workspace
   int split_keys;    // keys per split (the last one takes all that is left)

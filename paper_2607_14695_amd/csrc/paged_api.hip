@@ -230,7 +230,8 @@ int reflex_paged_attention(const reflex_paged_cache* cache, const reflex_paged_b
   a.n_rows = n_rows;
   a.n_q = n_q_heads;
   a.group = n_q_heads / cache->n_kv_heads;
-  a.scale2 = (float)((double)scale * 1.4426950408889634);
+  a.scale2 = (float)fmax(fabs((double)scale) * 1.4426950408889634, 1.1754943508222875e-38);
+  a.negate = scale < 0.f;
   a.causal = causal != 0;
   a.window = window;
   a.nsplit = p.nsplit;

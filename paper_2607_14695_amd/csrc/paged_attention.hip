@@ -50,7 +50,7 @@ RFX_DEV void scalar_row(const PagedAttnArgs& a, int64_t row, int head, int b, Sp
   float q[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    q[i] = to_f(qp[i]);
+    q[i] = a.negate ? -to_f(qp[i]) : to_f(qp[i]);
     o[i] = 0.f;
   }
   m = kFloor;
@@ -97,6 +97,19 @@ template <int N> RFX_DEV void wait_copies_if(bool newer) {
 // ---------------------------------------------------------------------------
 // shared pieces of the tiled kernels
 // ---------------------------------------------------------------------------
+// lds_dma16 from a wave-uniform base, with an offset added to both addresses
+template <int OFF> RFX_DEV void lds_dma16_at(const void* base, uint32_t off, void* lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3"
+               :: "v"(off), "s"(base), "s"((unsigned)(size_t)lds), "n"(OFF) : "memory");
+}
+
+template <int N, typename F> RFX_DEV void static_for(F&& f) {
+  if constexpr (N > 0) {
+    static_for<N - 1>(f);
+    f(std::integral_constant<int, N - 1>{});
+  }
+}
+
 template <int N> RFX_DEV void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 // LDS reads issued so far have their values: what they read may be overwritten
 RFX_DEV void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
@@ -132,6 +145,16 @@ RFX_DEV uint2 ld_tr16(const unsigned char* lds) {
 }
 RFX_DEV uint2 ld_tr8(const unsigned char* lds) {
   return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((RFX_LDS i32x2_v*)lds));
+}
+
+// a fragment, or its negative
+RFX_DEV uint4 signed_frag(uint4 v, int negate, bf16_t) {
+  const uint32_t f = negate ? 0x80008000u : 0u;
+  return make_uint4(v.x ^ f, v.y ^ f, v.z ^ f, v.w ^ f);
+}
+RFX_DEV uint4 signed_frag(uint4 v, int negate, float) {
+  const uint32_t f = negate ? 0x80000000u : 0u;
+  return make_uint4(v.x ^ f, v.y ^ f, v.z ^ f, v.w ^ f);
 }
 
 RFX_DEV uint32_t pack_bf16(float a, float b) {
@@ -326,7 +349,7 @@ __global__ __launch_bounds__(256) void paged_attn_few_kernel(const PagedAttnArgs
       if (!Q8) d = QS * k + (QS / 4) * g;
       else if (BF) d = 64 * (k >> 1) + 16 * g + 8 * (k & 1);
       else d = 64 * (k >> 2) + 16 * g + 4 * (k & 3);
-      qf[m][k] = r < t.rows ? ld16(qp + d) : zero16();
+      qf[m][k] = r < t.rows ? signed_frag(ld16(qp + d), a.negate, T(0)) : zero16();
     }
   }
   f32x4_v o[MR][NDB];
@@ -624,8 +647,15 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
   constexpr bool Q8 = C::Q8;
   constexpr int KT = C::KT, RB = C::RB, NCH = C::NCH, NI = C::NI, RPC = C::RPC, TB = C::TB;
   constexpr int NKS = DH / 16, NDB = DH / 32, BM = 128, OP = DH + 4;
+  constexpr int NKH = NCH / 2;  // K reads of a row: 32 bytes each, two lanes' chunks
+  constexpr int T2 = DH / 8;                  // products of a tile's scores, and of its values
+  constexpr int KA = DH > 128 ? 4 : 2;        // K reads under way, of each block of 32 keys
+  constexpr int VA = 4;                       // V fragments under way
+  // 256-wide heads run one wave per SIMD, with accumulators in the upper half
+  // of the registers
+  constexpr bool WIDE = DH > 128;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[C::SMEM];
-  __shared__ float scales[2][2][KT];
+  __shared__ float scales[2][4][KT];  // a ring of four tiles' K scales, and of V's
   __shared__ int table[C::kTable];
   __shared__ float2 ml[BM];
 
@@ -664,7 +694,7 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
 #pragma unroll
     for (int k = 0; k < NKS; ++k) {
       const int d = Q8 ? 32 * (k >> 1) + 16 * h + 8 * (k & 1) : 16 * k + 8 * h;
-      qf[k] = r < t.rows ? ld16(qp + d) : zero16();
+      qf[k] = r < t.rows ? signed_frag(ld16(qp + d), a.negate, T(0)) : zero16();
     }
   }
   f32x16_v o[NDB];
@@ -677,7 +707,7 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
   const char *const pk = a.c.k, *const pv = a.c.v;
   const float *const psk = a.c.k_scale, *const psv = a.c.v_scale;
   const float scale2 = a.scale2;
-  const bool in_page = (1 << shift) >= RPC;  // the rows of a copy lie in one page
+  const bool in_page = (1 << shift) >= KT / 4;  // the rows a wave copies lie in one page
   // Swizzles of the 16-byte chunks of a row in LDS: K reads take one chunk of
   // 32 rows at a time, V reads 64 bytes of 8 rows.  They are XORs, and rows
   // are powers of two apart, so the address of every read is one of few
@@ -698,11 +728,15 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
       vreg[d] = 2 * TB + row * RB + ((ch ^ swv(row)) << 4) + (i16 & 1) * 8;
     }
   }
-  // this lane's offset within its wave's first copy of a tile; the swizzle of
-  // the others differs by a constant
+  // this lane's offset within its wave's copies of a tile, four at a time
   const int sub = lane / NCH;
-  const uint32_t koff = sub * RB + (((lane % NCH) ^ swk(sub)) << 4);
-  const uint32_t voff = sub * RB + (((lane % NCH) ^ swv(sub)) << 4);
+  constexpr int NO = NI < 4 ? NI : 4;
+  uint32_t koff[NO], voff[NO];
+#pragma unroll
+  for (int j = 0; j < NO; ++j) {
+    koff[j] = sub * RB + (((lane % NCH) ^ swk(j * RPC + sub)) << 4);
+    voff[j] = sub * RB + (((lane % NCH) ^ swv(j * RPC + sub)) << 4);
+  }
 
   for (int seg = k_beg & ~(KT - 1); seg < k_end;) {
     const int e0 = seg >> shift;
@@ -724,192 +758,293 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
       const int pg = table[(min(key, seg_end - 1) >> shift) - e0];
       return key < k_beg || key >= seg_end || pg < 0 ? -1 : ((pg * n_kv) << shift) + (key & ((1 << shift) - 1));
     };
-    // rr: the lane's page row.  Mostly all 64 are there and a copy's rows lie in
-    // one page: then only a uniform base and the lane's offset are needed.
-    auto copy = [&](const char* base, auto sw, uint32_t off, int rr, unsigned char* dst) __attribute__((always_inline)) {
-      if (in_page && !__ballot(rr < 0)) {
-#pragma unroll
-        for (int j = 0; j < NI; ++j) {
-          const int pr = __builtin_amdgcn_readlane(rr, (wave * NI + j) * RPC);
-          lds_dma16(base + ((int64_t)pr + hoff) * RB, off ^ (sw(j * RPC) << 4), dst + (wave * NI + j) * 1024);
-        }
-      } else {
+    // A tile's copies; rr: the lane's page row of it.  Mostly all 64 are there
+    // and the 16 rows that a wave copies lie in one page (`plain`): then they
+    // are one run of bytes, and copy j needs the run's base and the lane's
+    // offset.
+    auto plain = [&](int rr) __attribute__((always_inline)) { return in_page && !__ballot(rr < 0); };
+    auto run_of = [&](const char* base, int rr) __attribute__((always_inline)) {
+      return base + ((int64_t)__builtin_amdgcn_readlane(rr, wave * (KT / 4)) + hoff) * RB;
+    };
+    auto copy_one = [&](const char* run, auto sw, const uint32_t (&off)[NO], unsigned char* dst, auto J)
+        __attribute__((always_inline)) {
+      constexpr int j = decltype(J)::value;
+      // (copies four apart: the swizzle's bits beyond those of four copies)
+      const uint32_t o = j < 4 ? off[j % NO] : off[j % NO] ^ ((sw(j * RPC) ^ sw(j % 4 * RPC)) << 4);
+      lds_dma16_at<(j & 3) * 1024>(run + (j >> 2) * 4096, o, dst + wave * NI * 1024 + (j >> 2) * 4096);
+    };
+    auto copy_any = [&](const char* base, auto sw, int rr, unsigned char* dst) __attribute__((always_inline)) {
 #pragma unroll 1
-        for (int j = 0; j < NI; ++j) {
-          const int pr = __shfl(rr, (wave * NI + j) * RPC + sub, 64);
-          const char* src = base + ((int64_t)pr + hoff) * RB + ((off ^ (sw(j * RPC) << 4)) - sub * RB);
-          lds_dma16(pr < 0 ? reinterpret_cast<const char*>(kZeros) : src, dst + (wave * NI + j) * 1024);
-        }
+      for (int j = 0; j < NI; ++j) {
+        const int row = j * RPC + sub;
+        const int pr = __shfl(rr, wave * (KT / 4) + row, 64);
+        const char* src = base + ((int64_t)pr + hoff) * RB + (((lane % NCH) ^ sw(row)) << 4);
+        lds_dma16(pr < 0 ? reinterpret_cast<const char*>(kZeros) : src, dst + (wave * NI + j) * 1024);
       }
     };
-    auto copy_k = [&](int x, int buf) __attribute__((always_inline)) {
-      const int rr = row_of(x);
-      copy(pk, swk, koff, rr, smem + buf * TB);
+    // scales of tile x, two steps before its values are taken
+    auto copy_scales = [&](int rr, int x) __attribute__((always_inline)) {
+      if (Q8 && wave < 2) lds_dma4((wave == 0 ? psk : psv) + max(rr, 0) + hoff, scales[wave][x & 3]);
     };
-    // (with the scales of the tile's keys: the softmax reads them while K of
-    // two tiles further is on its way)
-    auto copy_v = [&](int x, int buf) __attribute__((always_inline)) {
-      const int rr = row_of(x);
-      copy(pv, swv, voff, rr, smem + (2 + buf) * TB);
-      if (Q8 && wave < 2) lds_dma4((wave == 0 ? psk : psv) + max(rr, 0) + hoff, scales[wave][buf]);
-    };
-    // S^T of a tile: block b, register i holds key 32 b + 8 (i / 4) + 4 h + i % 4
-    auto scores = [&](uint32_t buf, f32x16_v (&s)[2]) __attribute__((always_inline)) {
-      s[0] = f32x16_v{};
-      s[1] = f32x16_v{};
+    // S^T of a tile: block b, register i holds key 32 b + 8 (i / 4) + 4 h + i % 4.
+    // K fragments are requested KA steps ahead.
+    auto k_load = [&](uint32_t buf, int k, uint4 (&kf)[KA][2]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int k = 0; k < NCH / 2; ++k)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const uint4 c = ld16(smem + kreg[k % NKR] + buf + (k / NKR) * 256 + b * 32 * RB);
-          if (!Q8) {
-            mfma32_step(s[b], c, qf[k]);
-          } else {
-            mfma32_step(s[b], codes_to_bf16<ST>(make_uint2(c.x, c.y)), qf[2 * k]);
-            mfma32_step(s[b], codes_to_bf16<ST>(make_uint2(c.z, c.w)), qf[2 * k + 1]);
-          }
-        }
+      for (int b = 0; b < 2; ++b)
+        kf[k % KA][b] = ld16(smem + (kreg[k % NKR] ^ buf) + (k / NKR) * 256 + b * 32 * RB);
     };
-    auto softmax = [&](int x, int buf, f32x16_v (&s)[2], uint4 (&pf)[4]) __attribute__((always_inline)) {
+    // product g of the scores: block g % 2, head dims 16 (g / 2) ..
+    auto k_mfma = [&](int g, const uint4 (&kf)[KA][2], f32x16_v (&s)[2]) __attribute__((always_inline)) {
+      const int b = g & 1, k = g >> 1;
+      if (!Q8) {
+        mfma32_step(s[b], kf[k % KA][b], qf[k]);
+      } else {
+        const uint4 c = kf[(k >> 1) % KA][b];
+        mfma32_step(s[b], codes_to_bf16<ST>(k & 1 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y)), qf[k]);
+      }
+    };
+    // O^T += V^T P^T: fragment n = u * NDB + d, step u covers keys 16 u + {4 h ..,
+    // 8 + 4 h ..}; requested VA ahead
+    auto v_load = [&](uint32_t buf, int n, uint4 (&vf)[VA]) __attribute__((always_inline)) {
+      const int u = n / NDB, d = n % NDB;
+      if (Q8) {
+        const uint2 c = ld_tr8(smem + (vreg[d % NVR] ^ buf) + 16 * u * RB);
+        vf[n % VA] = make_uint4(c.x, c.y, 0u, 0u);
+      } else {
+        // rows 8 further: the swizzle differs by 16 of the chunk's bits, if it has that many
+        const unsigned char* at = smem + (vreg[d % NVR] ^ buf) + 16 * u * RB;
+        constexpr int flip = NCH > 16 ? 1 : 0;
+        const uint2 f0 = ld_tr16(at + (d / NVR) * 256), f1 = ld_tr16(at + 8 * RB + ((d / NVR) ^ flip) * 256);
+        vf[n % VA] = make_uint4(f0.x, f0.y, f1.x, f1.y);
+      }
+    };
+    auto v_mfma = [&](int n, const uint4 (&vf)[VA], const uint4& pf) __attribute__((always_inline)) {
+      const uint4 f = vf[n % VA];
+      mfma32_step(o[n % NDB], Q8 ? codes_to_bf16<ST>(make_uint2(f.x, f.y)) : f, pf);
+    };
+
+    // the softmax in pieces.  Scores stay as the product left them (times the
+    // keys' scales); `scale2` enters with the maximum's subtraction.
+    auto is_whole = [&](int x) __attribute__((always_inline)) {
       const int key0 = seg + x * KT;
-      const bool whole = seg_ok && key0 >= all_lo && key0 + KT <= all_hi && key0 + KT <= seg_end;
+      return seg_ok && key0 >= all_lo && key0 + KT <= all_hi && key0 + KT <= seg_end;
+    };
+    auto key_scales = [&](int x, f32x16_v (&s)[2]) __attribute__((always_inline)) {
       if (Q8) {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float4 k4 = *reinterpret_cast<const float4*>(&scales[0][buf][32 * b + 8 * i + 4 * h]);
+            const float4 k4 = *reinterpret_cast<const float4*>(&scales[0][x & 3][32 * b + 8 * i + 4 * h]);
             s[b][4 * i] *= k4.x; s[b][4 * i + 1] *= k4.y; s[b][4 * i + 2] *= k4.z; s[b][4 * i + 3] *= k4.w;
           }
       }
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[b][i] *= scale2;
-      if (!whole) {
-        const int l0 = lo - key0 - 4 * h, h0 = min(hi, seg_end) - key0 - 4 * h;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int at = 32 * b + 8 * (i >> 2) + (i & 3);
-            s[b][i] = at >= l0 && at < h0 ? s[b][i] : -INFINITY;
-          }
-        if (!seg_ok) {
-          const uint64_t present = __ballot(row_of(x) >= 0) >> (4 * h);
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (!((present >> (32 * b + 8 * (i >> 2) + (i & 3))) & 1)) s[b][i] = -INFINITY;
-        }
-      }
-      float top = kFloor;
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-      {
-        auto z = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-        top = fmaxf(__uint_as_float(z[0]), __uint_as_float(z[1]));
-      }
-      if (__ballot(top > mx + kSlack)) {
-        const float nm = top > mx + kSlack ? top : mx;
-        const float f = __builtin_amdgcn_exp2f(mx - nm);
-        mx = nm;
-        sum *= f;
-#pragma unroll
-        for (int d = 0; d < NDB; ++d) o[d] *= f;
-      }
-      float add = 0.f;
+    };
+    auto mask = [&](int x, f32x16_v (&s)[2]) __attribute__((always_inline)) {
+      const int key0 = seg + x * KT;
+      const int l0 = lo - key0 - 4 * h, h0 = min(hi, seg_end) - key0 - 4 * h;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float p = __builtin_amdgcn_exp2f(s[b][i] - mx);
-          add += p;
-          s[b][i] = p;
+          const int at = 32 * b + 8 * (i >> 2) + (i & 3);
+          s[b][i] = at >= l0 && at < h0 ? s[b][i] : -INFINITY;
         }
-      sum += add;
-      if (Q8) {
+      if (!seg_ok) {
+        const uint64_t present = __ballot(row_of(x) >= 0) >> (4 * h);
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 v4 = *reinterpret_cast<const float4*>(&scales[1][buf][32 * b + 8 * i + 4 * h]);
-            const float vv[4] = {v4.x, v4.y, v4.z, v4.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float p = s[b][4 * i + e];
-              // (a key that the row does not see may have any scale)
-              s[b][4 * i + e] = whole || p > 0.f || p != p ? p * vv[e] : 0.f;
-            }
-          }
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const f32x16_v& v = s[u >> 1];
-        const int e = 8 * (u & 1);
-        pf[u] = make_uint4(pack_bf16(v[e], v[e + 1]), pack_bf16(v[e + 2], v[e + 3]), pack_bf16(v[e + 4], v[e + 5]),
-                           pack_bf16(v[e + 6], v[e + 7]));
+          for (int i = 0; i < 16; ++i)
+            if (!((present >> (32 * b + 8 * (i >> 2) + (i & 3))) & 1)) s[b][i] = -INFINITY;
       }
     };
-    // O^T += V^T P^T: step u covers keys 16 u + {4 h .., 8 + 4 h ..}
-    auto values = [&](uint32_t buf, const uint4 (&pf)[4]) __attribute__((always_inline)) {
+    auto block_max = [&](const f32x16_v& s) __attribute__((always_inline)) {
+      float m[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int d = 0; d < NDB; ++d) {
-          uint4 f;
-          if (Q8) {
-            f = codes_to_bf16<ST>(ld_tr8(smem + vreg[d] + buf + 16 * u * RB));
-          } else {
-            // rows 8 further: the swizzle differs by 16 of the chunk's bits, if it has that many
-            const unsigned char* at = smem + vreg[d % NVR] + buf + 16 * u * RB;
-            constexpr int flip = NCH > 16 ? 1 : 0;
-            const uint2 f0 = ld_tr16(at + (d / NVR) * 256), f1 = ld_tr16(at + 8 * RB + ((d / NVR) ^ flip) * 256);
-            f = make_uint4(f0.x, f0.y, f1.x, f1.y);
-          }
-          mfma32_step(o[d], f, pf[u]);
-        }
+      for (int i = 0; i < 4; ++i) m[i] = fmaxf(fmaxf(fmaxf(s[4 * i], s[4 * i + 1]), s[4 * i + 2]), s[4 * i + 3]);
+      return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
     };
+    // the row's maximum, in the unit of the exponent
+    auto row_top = [&](float top) __attribute__((always_inline)) {
+      auto z = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+      return fmaxf(fmaxf(__uint_as_float(z[0]), __uint_as_float(z[1])) * scale2, kFloor);
+    };
+    auto raise = [&](float top) __attribute__((always_inline)) {
+      const float nm = top > mx + kSlack ? top : mx;
+      const float f = __builtin_amdgcn_exp2f(mx - nm);
+      mx = nm;
+      sum *= f;
+#pragma unroll
+      for (int d = 0; d < NDB; ++d) o[d] *= f;
+    };
+    // probabilities of registers 2 (q % 8) and the next of block q / 8; the
+    // empty statement keeps them at their place among the products
+    auto pair = [&](int x, bool whole, int q, const f32x16_v (&s)[2], uint32_t (&pw)[16]) __attribute__((always_inline)) {
+      const int i = 2 * (q & 7);
+      float p0 = __builtin_amdgcn_exp2f(fmaf(s[q >> 3][i], scale2, -mx));
+      float p1 = __builtin_amdgcn_exp2f(fmaf(s[q >> 3][i + 1], scale2, -mx));
+      sum += p0 + p1;
+      if (Q8) {
+        const float2 v = *reinterpret_cast<const float2*>(&scales[1][x & 3][32 * (q >> 3) + 8 * (i >> 2) + 4 * h + (i & 3)]);
+        // (a key that the row does not see may have any scale)
+        p0 = whole || p0 > 0.f || p0 != p0 ? p0 * v.x : 0.f;
+        p1 = whole || p1 > 0.f || p1 != p1 ? p1 * v.y : 0.f;
+      }
+      pw[q] = pack_bf16(p0, p1);
+      asm volatile("" : "+v"(pw[q]), "+v"(sum));
+    };
+    auto pfrag = [](const uint32_t (&pw)[16], int u) __attribute__((always_inline)) {
+      return make_uint4(pw[4 * u], pw[4 * u + 1], pw[4 * u + 2], pw[4 * u + 3]);
+    };
+    auto fence = [&]() __attribute__((always_inline)) { __builtin_amdgcn_sched_barrier(0); };
     // all of the wave's copies have landed and its reads are done, in every wave
     auto turn = [&]() __attribute__((always_inline)) {
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     };
 
-    copy_k(0, 0);
-    copy_v(0, 0);
-    if (n_t > 1) copy_k(1, 1);
+    int rr1 = row_of(0);
+    copy_any(pk, swk, rr1, smem);
+    copy_any(pv, swv, rr1, smem + 2 * TB);
+    copy_scales(rr1, 0);
+    rr1 = row_of(1);  // page rows of tile x + 1 in the loop
+    copy_scales(rr1, 1);
+    if (n_t > 1) copy_any(pk, swk, rr1, smem + TB);
     turn();
     f32x16_v sa[2], sb[2];
-    scores(0, sa);
+    sa[0] = f32x16_v{};
+    sa[1] = f32x16_v{};
+    {
+      uint4 kf[KA][2];
+#pragma unroll
+      for (int k = 0; k < KA; ++k) k_load(0, k, kf);
+#pragma unroll
+      for (int g = 0; g < T2; ++g) {
+        k_mfma(g, kf, sa);
+        if ((Q8 ? g & 1 && g >> 1 & 1 : g & 1) && g / (T2 / NKH) + KA < NKH) k_load(0, g / (T2 / NKH) + KA, kf);
+      }
+    }
+    // scores of tile x as the softmax takes them; returns the rows' maxima
+    auto ready = [&](int x, f32x16_v (&s)[2]) __attribute__((always_inline)) {
+      key_scales(x, s);
+      if (!is_whole(x)) mask(x, s);
+      return row_top(fmaxf(block_max(s[0]), block_max(s[1])));
+    };
+    {
+      const float top = ready(0, sa);
+      if (__ballot(top > mx + kSlack)) raise(top);
+    }
     turn();
-    uint4 pf[4];
-    // one tile's softmax and values under the next one's scores and copies;
-    // B: the tile's buffers
-    auto step = [&](int x, auto B, f32x16_v (&cur)[2], f32x16_v (&nxt)[2]) __attribute__((always_inline)) {
-      constexpr int buf = decltype(B)::value;
-      if (x + 2 < n_t) copy_k(x + 2, buf);
-      copy_v(x + 1, buf ^ 1);
-      scores((buf ^ 1) * TB, nxt);
-      softmax(x, buf, cur, pf);
-      values(buf * TB, pf);
-      turn();
+    uint32_t pw[16];
+    // Step x: probabilities and values of tile x, scores of tile x + 1, copies
+    // of K of tile x + 2 and of V of tile x + 1.  The vector work lies between
+    // the products by hand; the fences keep it there.  Returns the maxima of
+    // the new scores.
+    auto step = [&](int x, f32x16_v (&cur)[2], f32x16_v (&nxt)[2]) __attribute__((always_inline)) {
+      const uint32_t bx = x & 1 ? TB : 0, by = TB - bx;
+      const bool whole = is_whole(x);
+      const int rr2 = row_of(x + 2);
+      uint4 kf[KA][2], vf[VA];
+#pragma unroll
+      for (int k = 0; k < KA; ++k) k_load(by, k, kf);
+      const bool easy = x + 2 < n_t && plain(rr1) && plain(rr2);
+      const char *run_k = run_of(pk, rr2), *run_v = run_of(pv, rr1);
+      unsigned char *const dk = smem + bx, *const dv = smem + 2 * TB + by;
+      if (!easy) {
+        if (x + 2 < n_t) copy_any(pk, swk, rr2, dk);
+        copy_any(pv, swv, rr1, dv);
+      }
+      copy_scales(rr2, x + 2);
+      nxt[0] = f32x16_v{};
+      nxt[1] = f32x16_v{};
+      fence();
+      // what goes with product g of the tile's 2 T2
+      auto beside = [&](auto G) __attribute__((always_inline)) {
+        constexpr int g = decltype(G)::value;
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+          if (g == T2 / 16 + q * 11 * T2 / 128) pair(x, whole, q, cur, pw);
+        // copies over the first three quarters
+        constexpr int STEP = 3 * T2 / 2 / (2 * NI);
+        if constexpr (g % STEP == STEP - 1 && g / STEP < 2 * NI) {
+          constexpr int c = g / STEP;
+          if (easy) {
+            if constexpr (c < NI) copy_one(run_k, swk, koff, dk, std::integral_constant<int, c>{});
+            else copy_one(run_v, swv, voff, dv, std::integral_constant<int, c - NI>{});
+          }
+        }
+      };
+      static_for<T2>([&](auto G) __attribute__((always_inline)) {
+        constexpr int g = decltype(G)::value;
+        constexpr int per = T2 / NKH;  // products to a K read of both blocks
+        k_mfma(g, kf, nxt);
+        if constexpr (g % per == per - 1 && g / per + KA < NKH) k_load(by, g / per + KA, kf);
+        if constexpr (g == T2 - 1) {
+#pragma unroll
+          for (int n = 0; n < VA; ++n) v_load(bx, n, vf);
+        }
+        beside(G);
+        fence();
+      });
+      static_for<T2>([&](auto N) __attribute__((always_inline)) {
+        constexpr int n = decltype(N)::value;
+        v_mfma(n, vf, pfrag(pw, n / NDB));
+        if constexpr (n + VA < T2) v_load(bx, n + VA, vf);
+        beside(std::integral_constant<int, T2 + n>{});
+        fence();
+      });
+      rr1 = rr2;
+      return ready(x + 1, nxt);
     };
     int x = 0;
-    for (; x + 2 < n_t; x += 2) {
-      step(x, std::integral_constant<int, 0>{}, sa, sb);
-      step(x + 1, std::integral_constant<int, 1>{}, sb, sa);
+    if constexpr (WIDE) {
+      // the loop without a rescaling: one within it would move the
+      // accumulators about at every turn
+      while (x + 1 < n_t) {
+        float top;
+        bool high;
+        do {
+          top = step(x, sa, sb);
+          turn();
+          sa[0] = sb[0];
+          sa[1] = sb[1];
+          high = __ballot(top > mx + kSlack) != 0;
+          ++x;
+        } while (x + 1 < n_t && !high);
+        if (high) raise(top);
+      }
+    } else {
+      for (; x + 2 < n_t; x += 2) {
+        float top = step(x, sa, sb);
+        if (__ballot(top > mx + kSlack)) raise(top);
+        turn();
+        top = step(x + 1, sb, sa);
+        if (__ballot(top > mx + kSlack)) raise(top);
+        turn();
+      }
+      if (x + 1 < n_t) {
+        const float top = step(x, sa, sb);
+        if (__ballot(top > mx + kSlack)) raise(top);
+        turn();
+        ++x;
+        sa[0] = sb[0];
+        sa[1] = sb[1];
+      }
     }
-    if (x + 1 < n_t) {
-      step(x, std::integral_constant<int, 0>{}, sa, sb);
-      ++x;
-      sa[0] = sb[0];
-      sa[1] = sb[1];
+    {
+      const uint32_t bx = x & 1 ? TB : 0;
+      const bool whole = is_whole(x);
+#pragma unroll
+      for (int q = 0; q < 16; ++q) pair(x, whole, q, sa, pw);
+      uint4 vf[VA];
+#pragma unroll
+      for (int n = 0; n < VA; ++n) v_load(bx, n, vf);
+#pragma unroll
+      for (int n = 0; n < T2; ++n) {
+        v_mfma(n, vf, pfrag(pw, n / NDB));
+        if (n + VA < T2) v_load(bx, n + VA, vf);
+      }
     }
-    softmax(x, x & 1, sa, pf);
-    values((x & 1) * TB, pf);
     seg = seg_end;
   }
 
