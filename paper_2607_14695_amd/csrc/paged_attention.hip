@@ -202,10 +202,12 @@ RFX_DEV bool find_tile(const PagedAttnArgs& a, int tile, int bm, int lane, Tile&
   int before = 0;
   for (int b0 = 0; b0 < a.q.n; b0 += 64) {
     const int b = b0 + lane;
-    int c0 = 0, c1 = 0;
+    int c0 = 0, c1 = 0, end = 0, len = 0;
     if (b < a.q.n) {
       c0 = (int)min((int64_t)max(a.q.cu[b], 0), a.n_rows);
-      c1 = (int)min((int64_t)max(a.q.cu[b + 1], 0), a.n_rows);
+      end = a.q.cu[b + 1];
+      c1 = (int)min((int64_t)max(end, 0), a.n_rows);
+      len = a.q.len[b];
     }
     const int mine = c1 > c0 ? ((c1 - c0) * a.group + bm - 1) / bm : 0;
     int sum = mine;
@@ -224,8 +226,8 @@ RFX_DEV bool find_tile(const PagedAttnArgs& a, int tile, int bm, int lane, Tile&
       t.r0 = __builtin_amdgcn_readfirstlane(t.r0);
       t.first_row = __builtin_amdgcn_readfirstlane(f0);
       t.rows = __builtin_amdgcn_readfirstlane((f1 - f0) * a.group);
-      t.len = __builtin_amdgcn_readfirstlane(a.q.len[t.b]);
-      t.first_pos = __builtin_amdgcn_readfirstlane((int)((int64_t)t.len - a.q.cu[t.b + 1] + f0));
+      t.len = __builtin_amdgcn_readfirstlane(__shfl(len, src, 64));
+      t.first_pos = __builtin_amdgcn_readfirstlane((int)((int64_t)t.len - __shfl(end, src, 64) + f0));
       return true;
     }
     before += __shfl(sum, 63, 64);
@@ -288,9 +290,9 @@ struct FewCfg {
   static constexpr bool Q8 = ST == REFLEX_STORE_FP8 || ST == REFLEX_STORE_INT8;
   static constexpr int ES = Q8 ? 1 : (int)sizeof(T);
   static constexpr int RB = DH * ES;                                          // bytes of a K or V row
-  static constexpr int KT = RB >= 1024 ? 16 : RB >= 512 ? 32 : 64;            // keys of a tile
+  static constexpr int KT = RB >= 1024 ? 16 : RB >= 256 ? 32 : 64;            // keys of a tile
   static constexpr int NCH = RB / 16;                                         // 16-byte chunks of a row
-  static constexpr int RPC = 64 / NCH;                                        // rows of a copy (0: half a row)
+  static constexpr int RPC = 64 / NCH;                                        // rows of a copy
   static constexpr int NI = KT * RB / 1024;                                   // copies of a tile
   static constexpr int TB = KT * RB;                                          // bytes of a tile
   static constexpr int SC = Q8 ? 2 * 64 * 4 : 0;                              // scales of a tile
@@ -298,8 +300,12 @@ struct FewCfg {
   static constexpr int kTable = 1024;                                         // page table entries held in LDS
 };
 
+// workgroups that a CU holds where their LDS allows it
 template <typename T, int ST, int DH, int MR>
-__global__ __launch_bounds__(256) void paged_attn_few_kernel(const PagedAttnArgs a) {
+constexpr int few_occupancy = MR == 1 && FewCfg<T, ST, DH>::WAVE <= 18 * 1024 ? 2 : 1;
+
+template <typename T, int ST, int DH, int MR>
+__global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_attn_few_kernel(const PagedAttnArgs a) {
   typedef FewCfg<T, ST, DH> C;
   constexpr bool Q8 = C::Q8, BF = sizeof(T) == 2;
   constexpr int KT = C::KT, RB = C::RB, NCH = C::NCH, NI = C::NI;
@@ -368,7 +374,21 @@ __global__ __launch_bounds__(256) void paged_attn_few_kernel(const PagedAttnArgs
   float* const vsc = ksc + 64;
   const int64_t hoff = (int64_t)kvh << a.c.shift;
   auto swz = [](int row) __attribute__((always_inline)) { return (Q8 ? row : 2 * row) & (NCH - 1); };
+  // copies after which the swizzle of a copy's rows repeats
+  constexpr int NSW = (Q8 ? NCH : NCH / 2) / C::RPC < 1 ? 1 : (Q8 ? NCH : NCH / 2) / C::RPC;
   const int shift = a.c.shift, n_pages = a.c.n_pages, n_kv = a.c.n_kv;
+  const char *const pk = a.c.k, *const pv = a.c.v;
+  const float *const psk = a.c.k_scale, *const psv = a.c.v_scale;
+  const float scale2 = a.scale2;
+  const bool in_page = (1 << shift) >= C::RPC;  // the rows of a copy lie in one page
+  // this lane's offset within copy j; the swizzle repeats after NO copies
+  constexpr int NO = NI < 1 ? 1 : NI < NSW ? NI : NSW;
+  uint32_t off[NO];
+#pragma unroll
+  for (int j = 0; j < NO; ++j) {
+    const int sub = lane / NCH;  // (rows of 1 KB: a copy is a row)
+    off[j] = sub * RB + (((lane % NCH) ^ swz(j * C::RPC + sub)) << 4);
+  }
 
   for (int seg = k_beg & ~(KT - 1); seg < k_end;) {
     // the segment's table entries, checked once: -1 where the page is absent
@@ -392,28 +412,39 @@ __global__ __launch_bounds__(256) void paged_attn_few_kernel(const PagedAttnArgs
       const int pg = table[(key >> shift) - e0];
       return pg < 0 ? -1 : ((pg * n_kv) << shift) + (key & ((1 << shift) - 1));
     };
-    // copy a tile's K or V; r: this lane's page row; zeros where it has none
-    auto copy = [&](const char* base, const float* sc, int r, unsigned char* dst, float* sdst)
+    // Copy a tile's K or V; r: this lane's page row; zeros where it has none.
+    // Mostly all rows are there and those of a copy lie in one page: then the
+    // copy needs only a uniform base and the lane's offset.
+    auto copy = [&](const char* base, const float* sc, int r, bool easy, unsigned char* dst, float* sdst)
         __attribute__((always_inline)) {
+      if (easy) {
 #pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        const int row = (j * 64 + lane) / NCH, ch = (lane + j * 64) % NCH;
-        const int pr = __shfl(r, row, 64);
-        const char* src = base + ((int64_t)pr + hoff) * RB + ((ch ^ swz(row)) << 4);
-        lds_dma16(pr < 0 ? reinterpret_cast<const char*>(kZeros) : src, dst + j * 1024);
+        for (int j = 0; j < NI; ++j)
+          lds_dma16(base + ((int64_t)__builtin_amdgcn_readlane(r, j * 64 / NCH) + hoff) * RB, off[j % NO], dst + j * 1024);
+      } else {
+#pragma unroll 4
+        for (int j = 0; j < NI; ++j) {
+          const int row = (j * 64 + lane) / NCH, ch = lane % NCH;
+          const int pr = __shfl(r, row, 64);
+          const char* src = base + ((int64_t)pr + hoff) * RB + ((ch ^ swz(row)) << 4);
+          lds_dma16(pr < 0 ? reinterpret_cast<const char*>(kZeros) : src, dst + j * 1024);
+        }
       }
       if (Q8) lds_dma4(sc + (int64_t)max(r, 0) + hoff, sdst);
     };
+    constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << KT) - 1;
     constexpr int NC = NI + (Q8 ? 1 : 0);
 
     int r_cur = row_of(wave);
     if (wave < n_t) {
-      copy(a.c.k, a.c.k_scale, r_cur, kb, ksc);
-      copy(a.c.v, a.c.v_scale, r_cur, vb, vsc);
+      const bool easy = in_page && __ballot(r_cur >= 0) == kAll;
+      copy(pk, psk, r_cur, easy, kb, ksc);
+      copy(pv, psv, r_cur, easy, vb, vsc);
     }
     for (int x = wave; x < n_t; x += 4) {
       const int r_next = row_of(x + 4);
       const bool more = x + 4 < n_t;
+      const bool easy = in_page && __ballot(r_next >= 0) == kAll;
       const int key0 = seg + x * KT;
       const uint64_t present = __ballot(r_cur >= 0);
       wait_copies<NC>();
@@ -459,11 +490,11 @@ __global__ __launch_bounds__(256) void paged_attn_few_kernel(const PagedAttnArgs
 #pragma unroll
       for (int b = 0; b < NKB; ++b) ks[b] = Q8 ? *reinterpret_cast<const float4*>(ksc + 16 * b + 4 * g) : make_float4(1.f, 1.f, 1.f, 1.f);
       wait_lds();
-      if (more) copy(a.c.k, a.c.k_scale, r_next, kb, ksc);
+      if (more) copy(pk, psk, r_next, easy, kb, ksc);
 
       // softmax: scores in units of log2 e
       const bool whole = key0 >= lo_max && key0 + KT <= hi_min && key0 + KT <= s_end && key0 >= s_beg &&
-                         present == (KT == 64 ? ~0ull : (1ull << KT) - 1);
+                         present == kAll;
 #pragma unroll
       for (int m = 0; m < MR; ++m) {
         float top = kFloor;
@@ -473,7 +504,7 @@ __global__ __launch_bounds__(256) void paged_attn_few_kernel(const PagedAttnArgs
           const float kk[4] = {ks[b].x, ks[b].y, ks[b].z, ks[b].w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            float v = s[m][b][i] * a.scale2;
+            float v = s[m][b][i] * scale2;
             if (Q8) v *= kk[i];
             if (!whole) {
               const int at = 16 * b + 4 * g + i, key = key0 + at;
@@ -568,7 +599,7 @@ __global__ __launch_bounds__(256) void paged_attn_few_kernel(const PagedAttnArgs
           }
       }
       wait_lds();
-      if (more) copy(a.c.v, a.c.v_scale, r_next, vb, vsc);
+      if (more) copy(pv, psv, r_next, easy, vb, vsc);
       r_cur = r_next;
     }
     seg = seg_end;
@@ -774,7 +805,7 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
       lds_dma16_at<(j & 3) * 1024>(run + (j >> 2) * 4096, o, dst + wave * NI * 1024 + (j >> 2) * 4096);
     };
     auto copy_any = [&](const char* base, auto sw, int rr, unsigned char* dst) __attribute__((always_inline)) {
-#pragma unroll 1
+#pragma unroll 4
       for (int j = 0; j < NI; ++j) {
         const int row = j * RPC + sub;
         const int pr = __shfl(rr, wave * (KT / 4) + row, 64);
@@ -1167,10 +1198,10 @@ PagedAttnPlan paged_attention_plan(const reflex_paged_cache& c, const reflex_pag
   const int64_t len = b.max_length > 0 && b.max_length < cap ? b.max_length : cap;
   const int bm = rows_of_tile(n_rows, b.n_seqs, group, dtype);
   const int64_t blocks = tile_bound(n_rows, b.n_seqs, group, bm) * c.n_kv_heads;
-  // few rows: enough workgroups for every CU four times over, each with 128
-  // keys at least; many rows: at most one round of workgroups
+  // few rows: enough workgroups for every CU four times over (twice with 32
+  // rows), each with 128 keys at least; many rows: at most one round of them
   const int64_t slots = c.head_dim > 128 && c.store < REFLEX_STORE_FP8 ? 256 : 512;
-  int64_t want = bm == 128 ? slots / blocks : (1024 + blocks - 1) / blocks;
+  int64_t want = bm == 128 ? slots / blocks : ((bm == 16 ? 1024 : 512) + blocks - 1) / blocks;
   want = std::min<int64_t>(want, (len + 127) / 128);
   want = std::min<int64_t>(want, std::min<int64_t>(kMaxSplits, 65535 / c.n_kv_heads));
   want = std::max<int64_t>(want, 1);
