@@ -6,6 +6,8 @@
 // make a row: its maximum is a few shuffles.  A thread goes over several heads
 // of its token where there are enough tokens, because the angles' sines are
 // the arithmetic of these kernels and belong to the token alone.
+#include <type_traits>
+
 #include "paged.h"
 
 namespace reflex {
@@ -32,6 +34,23 @@ RFX_DEV double turn_of(int64_t pos, double turns) {
   return t - rint(t);
 }
 
+// The turns of a thread's 8 pairs (8 g ..) at a row's positions; with no
+// positions every axis counts the token.  All axes' positions are loaded at
+// once, and the pair's one is selected.
+RFX_DEV void turns_of(const reflex_rotary& plan, const int64_t* pos, int64_t ps, int64_t row, int64_t tok, int g,
+                      double* f) {
+  int64_t p[REFLEX_MAX_AXES];
+#pragma unroll
+  for (int a = 0; a < REFLEX_MAX_AXES; ++a) p[a] = pos ? pos[(a < plan.n_axes ? a : 0) * ps + row] : tok;
+  const uint64_t axes = *reinterpret_cast<const uint64_t*>(plan.axis + 8 * g);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int a = (int)(axes >> (8 * i)) & 3;
+    const int64_t lo = a & 1 ? p[1] : p[0], hi = a & 1 ? p[3] : p[2];
+    f[i] = turn_of(a & 2 ? hi : lo, plan.turns[8 * g + i]);
+  }
+}
+
 // ---------------------------------------------------------------------------
 // rotary
 // ---------------------------------------------------------------------------
@@ -46,12 +65,12 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
   const int h0 = blockIdx.y * a.heads_per, h1 = min(a.n_heads, h0 + a.heads_per);
   const T* x = reinterpret_cast<const T*>(a.x.p) + row * a.x.rs + 8 * g;
   T* y = reinterpret_cast<T*>(const_cast<char*>(a.y.p)) + row * a.y.rs + 8 * g;
+  double f[8];
+  turns_of(a.plan, a.pos, a.ps, row, 0, g, f);
   float cs[8], sn[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int pair = 8 * g + i;
-    const double f = turn_of(a.pos[a.plan.axis[pair] * a.ps + row], a.plan.turns[pair]);
-    sincospif(2.f * (float)f, &sn[i], &cs[i]);
+    sincospif(2.f * (float)f[i], &sn[i], &cs[i]);
     if (a.inverse) sn[i] = -sn[i];
   }
   for (int h = h0; h < h1; ++h) {
@@ -84,15 +103,56 @@ RFX_DEV float odd_float(double x) {
   return f;
 }
 
-// x / scale to the nearest integer, ties to even: the product with the
-// reciprocal is within 2^-50 of the quotient, so only a quotient that close
-// to a border needs the division
+// Sine and cosine of a fraction of a turn in [-1/2, 1/2], to a few 2^-53: the
+// nearest quarter turn is taken off, and the series of both functions (sine to
+// x^15, cosine to x^16) holds the rest, |x| <= pi / 4, to 2^-54 of 1.
+RFX_DEV void sincos_turn(double f, double* sn, double* cs) {
+  const double q = rint(4.0 * f);
+  const double x = fma(q, -0.25, f) * 6.283185307179586477;
+  const double z = x * x;
+  double s = -1.0 / 1307674368000.0;
+  s = fma(s, z, 1.0 / 6227020800.0);
+  s = fma(s, z, -1.0 / 39916800.0);
+  s = fma(s, z, 1.0 / 362880.0);
+  s = fma(s, z, -1.0 / 5040.0);
+  s = fma(s, z, 1.0 / 120.0);
+  s = fma(s, z, -1.0 / 6.0);
+  s = fma(s * z, x, x);
+  double c = 1.0 / 20922789888000.0;
+  c = fma(c, z, -1.0 / 87178291200.0);
+  c = fma(c, z, 1.0 / 479001600.0);
+  c = fma(c, z, -1.0 / 3628800.0);
+  c = fma(c, z, 1.0 / 40320.0);
+  c = fma(c, z, -1.0 / 720.0);
+  c = fma(c, z, 1.0 / 24.0);
+  c = fma(c, z, -0.5);
+  c = fma(c, z, 1.0);
+  const int n = (int)q;  // -2 .. 2
+  const double a = n & 1 ? c : s, b = n & 1 ? s : c;
+  *sn = n & 2 ? -a : a;
+  *cs = (n + 1) & 2 ? -b : b;
+}
+
+// x / scale to the nearest integer, ties to even.  In 64 bits the product with
+// the reciprocal is within 2^-50 of the quotient, so only a quotient that close
+// to a border needs the division.
 RFX_DEV int code_int8(double x, double scale, double inv) {
   const double t = x * inv;
   double r = rint(t);
   if (fabs(fabs(t - r) - 0.5) < 1e-9) r = rint(x / scale);
   return max(-127, min(127, (int)r));
 }
+// In 32 bits the product is within 2^-15 of the quotient.
+RFX_DEV int code_int8(float x, float scale, float inv) {
+  const float t = x * inv;
+  float r = rintf(t);
+  if (fabsf(fabsf(t - r) - 0.5f) < 0x1p-14f) r = (float)rint((double)x / (double)scale);
+  return max(-127, min(127, (int)r));
+}
+
+// what the conversion to e4m3 rounds: x / scale exactly, or rounded to odd
+RFX_DEV float fp8_source(double x, double inv) { return odd_float(x * inv); }
+RFX_DEV float fp8_source(float x, float inv) { return x * inv; }
 
 // Scale of a row from the bits of its largest magnitude; NaN for a row with a
 // value that is not finite.
@@ -107,12 +167,13 @@ RFX_DEV float row_scale(uint32_t amax) {
   return __uint_as_float((uint32_t)(k + 127) << 23);
 }
 
-// The codes of 8 values as 8 bytes.
-template <int ST>
-RFX_DEV uint2 codes8(const double* x, float scale) {
+// The codes of 8 values as 8 bytes.  A rotated key comes in 64 bits (F =
+// double); other values are what they are in fp32.
+template <int ST, typename F>
+RFX_DEV uint2 codes8(const F* x, float scale) {
   uint32_t w[2] = {0, 0};
   if (!(scale < INFINITY)) return make_uint2(0u, 0u);
-  const double s = (double)scale, inv = 1.0 / s;
+  const F s = (F)scale, inv = F(1) / s;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     if (ST == REFLEX_STORE_INT8) {
@@ -121,7 +182,7 @@ RFX_DEV uint2 codes8(const double* x, float scale) {
     } else {
       float f[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) f[j] = fminf(fmaxf(odd_float(x[4 * i + j] * inv), -448.f), 448.f);  // inv: a power of two
+      for (int j = 0; j < 4; ++j) f[j] = fminf(fmaxf(fp8_source(x[4 * i + j], inv), -448.f), 448.f);  // inv: a power of two
       int v = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
       w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], v, true);
     }
@@ -129,105 +190,117 @@ RFX_DEV uint2 codes8(const double* x, float scale) {
   return make_uint2(w[0], w[1]);
 }
 
-// blockIdx.z: 0 = K (rotated), 1 = V.  A wave holds 64 / G whole rows.
-template <typename T, int ST>
+// Token and page row (head 0) of row row0 + lane, or -1 where there is none:
+// the sequence of the wave's first row, and for the others how many of the next
+// 64 begin at or before them, by halving over the lanes.  Lanes past `rows`
+// look at no table.
+RFX_DEV int rows_of_wave(const Pages& c, const Seqs& q, int64_t row0, int rows, int64_t n_rows, int lane, int64_t& tok) {
+  const int64_t row = row0 + lane;
+  const int s0 = seq_of_row(q, row0, lane);
+  const int nx = s0 + 1 + lane <= q.n ? q.cu[s0 + 1 + lane] : INT32_MAX;
+  int lo = 0;
+#pragma unroll
+  for (int step = 32; step > 0; step >>= 1)
+    if ((int64_t)__shfl(nx, lo + step - 1, 64) <= row) lo += step;
+  lo += (int64_t)__shfl(nx, lo, 64) <= row;
+  int b = s0 + lo;
+  if (lo == 64)
+    while (b < q.n && q.cu[b + 1] <= row) ++b;  // many empty sequences
+  tok = 0;
+  if (lane >= rows || row >= n_rows || b < 0 || b >= q.n) return -2;
+  tok = (int64_t)q.len[b] - q.cu[b + 1] + row;
+  return page_row(c, q, b, tok);
+}
+
+// blockIdx.z: 0 = K (rotated), 1 = V.  A wave takes U times 64 / G rows.
+template <typename T, int ST, int U>
 __global__ __launch_bounds__(256) void paged_write_kernel(const PagedWriteArgs a) {
   const int G = a.c.dh >> 4;  // 4, 8 or 16
   const int lane = threadIdx.x & 63;
-  const int g = lane & (G - 1);
-  const int R = 64 / G;  // rows of a wave
-  const int64_t row0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * R;
+  const int g = lane & (G - 1), sub = lane / G;
+  const int R = 64 / G;
+  const int64_t row0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * (R * U);
   if (row0 >= a.n_rows) return;
-  const int64_t row = row0 + lane / G;
-  // sequences of the wave's rows: that of the first one, and how many of the
-  // next 64 begin at or before each other row
-  const int s0 = seq_of_row(a.q, row0, lane);
-  const int nx = s0 + 1 + lane <= a.q.n ? a.q.cu[s0 + 1 + lane] : INT32_MAX;
-  int b = s0;
-  for (int j = 0; j < R; ++j) {
-    const int c = __popcll(__ballot((int64_t)nx <= row0 + j));
-    if (lane / G == j) b = s0 + c;
-  }
-  if (b == s0 + 64)
-    while (b < a.q.n && a.q.cu[b + 1] <= row) ++b;  // many empty sequences
+  int64_t wave_tok;
+  const int wave_at = rows_of_wave(a.c, a.q, row0, R * U, a.n_rows, lane, wave_tok);
   const bool is_k = blockIdx.z == 0;
   const int half = a.c.dh >> 1;
-  bool live = row < a.n_rows && b >= 0 && b < a.q.n;
-  int64_t tok = 0;
-  int at = -1;
-  if (live) {
-    tok = (int64_t)a.q.len[b] - a.q.cu[b + 1] + row;
-    at = page_row(a.c, a.q, b, tok);
-    live = at >= 0;
-  }
   const Rows& in = is_k ? a.k : a.v;
-  const T* x = reinterpret_cast<const T*>(in.p) + row * in.rs + 8 * g;
   char* const out = is_k ? a.c.k : a.c.v;
   float* const scales = is_k ? a.c.k_scale : a.c.v_scale;
   const bool rot = is_k && a.rotate;
   constexpr bool Q = ST == REFLEX_STORE_FP8 || ST == REFLEX_STORE_INT8;
-  double cs[8], sn[8];
-  if (rot && live) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int pair = 8 * g + i;
-      const double f = turn_of(a.pos ? a.pos[a.plan.axis[pair] * a.ps + row] : tok, a.plan.turns[pair]);
-      if (Q) {
-        sincospi(2.0 * f, &sn[i], &cs[i]);
-      } else {
-        float s1, c1;
-        sincospif(2.f * (float)f, &s1, &c1);
-        sn[i] = s1;
-        cs[i] = c1;
-      }
-    }
-  }
+  typedef typename std::conditional<Q, double, float>::type F;  // what a rotation is computed in
   const int h0 = blockIdx.y * a.heads_per, h1 = min(a.c.n_kv, h0 + a.heads_per);
-  for (int h = h0; h < h1; ++h) {
-    float u[8], w[8];
-    const int64_t prow = (int64_t)at + ((int64_t)h << a.c.shift);
-    if (live) {
-      ld8(x + h * in.hs, u);
-      ld8(x + h * in.hs + half, w);
+#pragma unroll 1
+  for (int it = 0; it < U; ++it) {
+    const int64_t row = row0 + it * R + sub;
+    const int at = __shfl(wave_at, it * R + sub, 64);
+    const int64_t tok = (int64_t)__shfl((long long)wave_tok, it * R + sub, 64);
+    const bool live = at >= 0;
+    const T* x = reinterpret_cast<const T*>(in.p) + row * in.rs + 8 * g;
+    F cs[8], sn[8];
+    if (rot && live) {
+      double f[8];
+      turns_of(a.plan, a.pos, a.ps, row, tok, g, f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (Q) sincos_turn(f[i], &sn[i], &cs[i]);
+        else sincospif(2.f * (float)f[i], &sn[i], &cs[i]);
+      }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] = w[i] = 0.f;
+      for (int i = 0; i < 8; ++i) cs[i] = sn[i] = F(0);
     }
-    if (!Q) {
-      if (rot && live) {
+    for (int h = h0; h < h1; ++h) {
+      float u[8], w[8];
+      const int64_t prow = (int64_t)at + ((int64_t)h << a.c.shift);
+      if (live) {
+        ld8(x + h * in.hs, u);
+        ld8(x + h * in.hs + half, w);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = w[i] = 0.f;
+      }
+      auto put = [&](const auto* p, const auto* q) __attribute__((always_inline)) {
+        uint32_t amax = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          amax = max(amax, max(__float_as_uint((float)p[i]) & 0x7fffffffu, __float_as_uint((float)q[i]) & 0x7fffffffu));
+        for (int o = 1; o < G; o <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o, 64));
+        if (live) {
+          const float scale = row_scale<ST>(amax);
+          char* y = out + prow * a.c.dh + 8 * g;
+          *reinterpret_cast<uint2*>(y) = codes8<ST>(p, scale);
+          *reinterpret_cast<uint2*>(y + half) = codes8<ST>(q, scale);
+          if (g == 0) scales[prow] = scale;
+        }
+      };
+      if (rot) {
+        F p[8], q[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float c = (float)cs[i], s = (float)sn[i], p = u[i] * c - w[i] * s;
-          w[i] = w[i] * c + u[i] * s;
-          u[i] = p;
+          p[i] = (F)u[i] * cs[i] - (F)w[i] * sn[i];
+          q[i] = (F)w[i] * cs[i] + (F)u[i] * sn[i];
+        }
+        if constexpr (Q) {
+          put(p, q);
+          continue;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            u[i] = p[i];
+            w[i] = q[i];
+          }
         }
       }
-      if (live) {
+      if constexpr (Q) {
+        put(u, w);
+      } else if (live) {
         T* y = reinterpret_cast<T*>(out) + prow * a.c.dh + 8 * g;
         st8(y, u);
         st8(y + half, w);
       }
-      continue;
-    }
-    double p[8], q[8];
-    uint32_t amax = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = u[i];
-      q[i] = w[i];
-      if (rot && live) {
-        p[i] = (double)u[i] * cs[i] - (double)w[i] * sn[i];
-        q[i] = (double)w[i] * cs[i] + (double)u[i] * sn[i];
-      }
-      amax = max(amax, max(__float_as_uint((float)p[i]) & 0x7fffffffu, __float_as_uint((float)q[i]) & 0x7fffffffu));
-    }
-    for (int o = 1; o < G; o <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o, 64));
-    if (live) {
-      const float scale = row_scale<ST>(amax);
-      char* y = out + prow * a.c.dh + 8 * g;
-      *reinterpret_cast<uint2*>(y) = codes8<ST>(p, scale);
-      *reinterpret_cast<uint2*>(y + half) = codes8<ST>(q, scale);
-      if (g == 0) scales[prow] = scale;
     }
   }
 }
@@ -252,51 +325,59 @@ RFX_DEV void decode8(const uint2& c, float scale, float* o) {
   }
 }
 
-// blockIdx.z: 0 = K, 1 = V; blockIdx.y: the head.  Rows as in the writer.
-template <typename T, int ST>
+// blockIdx.z: 0 = K, 1 = V; blockIdx.y: the head.  A wave takes U times 64 / G
+// rows, whose loads are all under way before the first is used.
+template <typename T, int ST, int U>
 __global__ __launch_bounds__(256) void paged_read_kernel(const PagedReadArgs a) {
+  constexpr bool Q = ST == REFLEX_STORE_FP8 || ST == REFLEX_STORE_INT8;
   const int G = a.c.dh >> 4;
   const int lane = threadIdx.x & 63;
-  const int g = lane & (G - 1);
+  const int g = lane & (G - 1), sub = lane / G;
   const int R = 64 / G;
-  const int64_t row0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * R;
+  const int64_t row0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * (R * U);
   if (row0 >= a.n_rows) return;
-  const int64_t row = row0 + lane / G;
-  const int s0 = seq_of_row(a.q, row0, lane);
-  const int nx = s0 + 1 + lane <= a.q.n ? a.q.cu[s0 + 1 + lane] : INT32_MAX;
-  int b = s0;
-  for (int j = 0; j < R; ++j) {
-    const int c = __popcll(__ballot((int64_t)nx <= row0 + j));
-    if (lane / G == j) b = s0 + c;
-  }
-  if (b == s0 + 64)
-    while (b < a.q.n && a.q.cu[b + 1] <= row) ++b;
-  if (row >= a.n_rows || b < 0 || b >= a.q.n) return;
-  const int64_t tok = (int64_t)a.q.len[b] - a.q.cu[b + 1] + row;
-  const int at = page_row(a.c, a.q, b, tok);
+  int64_t tok;
+  const int wave_at = rows_of_wave(a.c, a.q, row0, R * U, a.n_rows, lane, tok);
   const bool is_k = blockIdx.z == 0;
   const int half = a.c.dh >> 1, h = blockIdx.y;
   const Rows& dst = is_k ? a.k : a.v;
-  T* y = reinterpret_cast<T*>(const_cast<char*>(dst.p)) + row * dst.rs + h * dst.hs + 8 * g;
-  float u[8], w[8];
+  const char* src = is_k ? a.c.k : a.c.v;
+  const float* scales = is_k ? a.c.k_scale : a.c.v_scale;
+  int at[U];
+  float u[U][8], w[U][8], scale[U];
+  uint2 c[U][2];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) u[i] = w[i] = 0.f;
-  if (at >= 0) {
-    const int64_t prow = (int64_t)at + ((int64_t)h << a.c.shift);
-    const char* src = is_k ? a.c.k : a.c.v;
-    if (ST == REFLEX_STORE_FP8 || ST == REFLEX_STORE_INT8) {
-      const float scale = (is_k ? a.c.k_scale : a.c.v_scale)[prow];
+  for (int i = 0; i < U; ++i) {
+    at[i] = __shfl(wave_at, i * R + sub, 64);
+    // (an absent row loads what its first head's page begins with)
+    const int64_t prow = (int64_t)max(at[i], 0) + ((int64_t)h << a.c.shift);
+    if (Q) {
+      scale[i] = scales[prow];
       const char* p = src + prow * a.c.dh + 8 * g;
-      decode8<ST>(*reinterpret_cast<const uint2*>(p), scale, u);
-      decode8<ST>(*reinterpret_cast<const uint2*>(p + half), scale, w);
+      c[i][0] = *reinterpret_cast<const uint2*>(p);
+      c[i][1] = *reinterpret_cast<const uint2*>(p + half);
     } else {
       const T* p = reinterpret_cast<const T*>(src) + prow * a.c.dh + 8 * g;
-      ld8(p, u);
-      ld8(p + half, w);
+      ld8(p, u[i]);
+      ld8(p + half, w[i]);
     }
   }
-  st8(y, u);
-  st8(y + half, w);
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    if (at[i] == -2) continue;  // of no sequence
+    if (Q) {
+      decode8<ST>(c[i][0], scale[i], u[i]);
+      decode8<ST>(c[i][1], scale[i], w[i]);
+    }
+    if (at[i] < 0) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[i][e] = w[i][e] = 0.f;
+    }
+    const int64_t row = row0 + i * R + sub;
+    T* y = reinterpret_cast<T*>(const_cast<char*>(dst.p)) + row * dst.rs + h * dst.hs + 8 * g;
+    st8(y, u[i]);
+    st8(y + half, w[i]);
+  }
 }
 
 // Heads a thread goes over: all of them where the tokens alone fill the chip
@@ -322,20 +403,28 @@ hipError_t launch_rotary(const RotaryArgs& args, hipStream_t s) {
 template hipError_t launch_rotary<float>(const RotaryArgs&, hipStream_t);
 template hipError_t launch_rotary<bf16_t>(const RotaryArgs&, hipStream_t);
 
+// Rows of a wave, in units of 64 / G: four where that still fills the chip.
+int pick_unroll(int64_t threads) { return threads >= 4 * 256 * 1024 ? 4 : 1; }
+
 template <typename T>
 hipError_t launch_paged_write(const PagedWriteArgs& args, int store, hipStream_t s) {
   PagedWriteArgs a = args;
   const int G = a.c.dh >> 4;
-  const int rows_per_block = 4 * (64 / G);
   a.heads_per = pick_heads_per(2 * a.n_rows * G, a.c.n_kv);
-  const dim3 grid((unsigned)((a.n_rows + rows_per_block - 1) / rows_per_block),
-                  (a.c.n_kv + a.heads_per - 1) / a.heads_per, 2);
-  if (store == REFLEX_STORE_FP8)
-    RFX_LAUNCH((paged_write_kernel<T, REFLEX_STORE_FP8>), grid, dim3(256), 0, s, a);
-  else if (store == REFLEX_STORE_INT8)
-    RFX_LAUNCH((paged_write_kernel<T, REFLEX_STORE_INT8>), grid, dim3(256), 0, s, a);
-  else
-    RFX_LAUNCH((paged_write_kernel<T, REFLEX_STORE_F32>), grid, dim3(256), 0, s, a);
+  const unsigned heads = (a.c.n_kv + a.heads_per - 1) / a.heads_per;
+  const int U = pick_unroll(2 * a.n_rows * G * heads);
+  const int rows_per_block = 4 * (64 / G) * U;
+  const dim3 grid((unsigned)((a.n_rows + rows_per_block - 1) / rows_per_block), heads, 2);
+  auto go = [&](auto S) {
+    constexpr int ST = decltype(S)::value;
+    if (U == 4)
+      RFX_LAUNCH((paged_write_kernel<T, ST, 4>), grid, dim3(256), 0, s, a);
+    else
+      RFX_LAUNCH((paged_write_kernel<T, ST, 1>), grid, dim3(256), 0, s, a);
+  };
+  if (store == REFLEX_STORE_FP8) go(std::integral_constant<int, REFLEX_STORE_FP8>{});
+  else if (store == REFLEX_STORE_INT8) go(std::integral_constant<int, REFLEX_STORE_INT8>{});
+  else go(std::integral_constant<int, REFLEX_STORE_F32>{});  // (the inputs' own type)
   return hipGetLastError();
 }
 template hipError_t launch_paged_write<float>(const PagedWriteArgs&, int, hipStream_t);
@@ -343,14 +432,20 @@ template hipError_t launch_paged_write<bf16_t>(const PagedWriteArgs&, int, hipSt
 
 template <typename T>
 hipError_t launch_paged_read(const PagedReadArgs& a, int store, hipStream_t s) {
-  const int rows_per_block = 4 * (64 / (a.c.dh >> 4));
+  const int G = a.c.dh >> 4;
+  const int U = pick_unroll(2 * a.n_rows * G * a.c.n_kv);
+  const int rows_per_block = 4 * (64 / G) * U;
   const dim3 grid((unsigned)((a.n_rows + rows_per_block - 1) / rows_per_block), a.c.n_kv, 2);
-  if (store == REFLEX_STORE_FP8)
-    RFX_LAUNCH((paged_read_kernel<T, REFLEX_STORE_FP8>), grid, dim3(256), 0, s, a);
-  else if (store == REFLEX_STORE_INT8)
-    RFX_LAUNCH((paged_read_kernel<T, REFLEX_STORE_INT8>), grid, dim3(256), 0, s, a);
-  else
-    RFX_LAUNCH((paged_read_kernel<T, REFLEX_STORE_F32>), grid, dim3(256), 0, s, a);
+  auto go = [&](auto S) {
+    constexpr int ST = decltype(S)::value;
+    if (U == 4)
+      RFX_LAUNCH((paged_read_kernel<T, ST, 4>), grid, dim3(256), 0, s, a);
+    else
+      RFX_LAUNCH((paged_read_kernel<T, ST, 1>), grid, dim3(256), 0, s, a);
+  };
+  if (store == REFLEX_STORE_FP8) go(std::integral_constant<int, REFLEX_STORE_FP8>{});
+  else if (store == REFLEX_STORE_INT8) go(std::integral_constant<int, REFLEX_STORE_INT8>{});
+  else go(std::integral_constant<int, REFLEX_STORE_F32>{});
   return hipGetLastError();
 }
 template hipError_t launch_paged_read<float>(const PagedReadArgs&, int, hipStream_t);
