@@ -190,27 +190,48 @@ RFX_DEV uint2 codes8(const F* x, float scale) {
   return make_uint2(w[0], w[1]);
 }
 
-// Token and page row (head 0) of row row0 + lane, or -1 where there is none:
-// the sequence of the wave's first row, and for the others how many of the next
-// 64 begin at or before them, by halving over the lanes.  Lanes past `rows`
-// look at no table.
+// Token and page row (head 0) of row row0 + lane: -2 where the row belongs to
+// no sequence, -1 where the token is absent.  Lanes past `rows` look at no
+// table.  Up to 63 sequences lie in the lanes themselves, with one load; of
+// more, the 64 after that of the wave's first row do.  A lane finds its own by
+// halving over them.
 RFX_DEV int rows_of_wave(const Pages& c, const Seqs& q, int64_t row0, int rows, int64_t n_rows, int lane, int64_t& tok) {
   const int64_t row = row0 + lane;
-  const int s0 = seq_of_row(q, row0, lane);
-  const int nx = s0 + 1 + lane <= q.n ? q.cu[s0 + 1 + lane] : INT32_MAX;
+  const bool few = q.n < 64;
+  const int first = few ? 0 : seq_of_row(q, row0, lane) + 1;
+  const int v = first + lane <= q.n ? q.cu[first + lane] : INT32_MAX;
+  const int ln = few && lane < q.n ? q.len[lane] : 0;
   int lo = 0;
 #pragma unroll
   for (int step = 32; step > 0; step >>= 1)
-    if ((int64_t)__shfl(nx, lo + step - 1, 64) <= row) lo += step;
-  lo += (int64_t)__shfl(nx, lo, 64) <= row;
-  int b = s0 + lo;
-  if (lo == 64)
-    while (b < q.n && q.cu[b + 1] <= row) ++b;  // many empty sequences
+    if ((int64_t)__shfl(v, lo + step - 1, 64) <= row) lo += step;
+  lo += (int64_t)__shfl(v, lo, 64) <= row;
+  int b = first + lo - 1;
+  int len = __shfl(ln, max(b, 0), 64), end = __shfl(v, min(lo, 63), 64);
   tok = 0;
+  if (!few && lo == 64)
+    while (b < q.n && q.cu[b + 1] <= row) ++b;  // many empty sequences
   if (lane >= rows || row >= n_rows || b < 0 || b >= q.n) return -2;
-  tok = (int64_t)q.len[b] - q.cu[b + 1] + row;
+  if (!few) {
+    len = q.len[b];
+    end = q.cu[b + 1];
+  }
+  tok = (int64_t)len - end + row;
   return page_row(c, q, b, tok);
 }
+
+// 8 elements as they lie in memory
+template <typename T> struct Raw8;
+template <> struct Raw8<float> {
+  uint4 a, b;
+  RFX_DEV void load(const float* p) { a = ld16(p); b = ld16(p + 4); }
+  RFX_DEV void to_f(float* o) const { frag_to_f(a, o, 0.f); frag_to_f(b, o + 4, 0.f); }
+};
+template <> struct Raw8<bf16_t> {
+  uint4 a;
+  RFX_DEV void load(const bf16_t* p) { a = ld16(p); }
+  RFX_DEV void to_f(float* o) const { frag_to_f(a, o, bf16_t(0)); }
+};
 
 // blockIdx.z: 0 = K (rotated), 1 = V.  A wave takes U times 64 / G rows.
 template <typename T, int ST, int U>
@@ -221,8 +242,6 @@ __global__ __launch_bounds__(256) void paged_write_kernel(const PagedWriteArgs a
   const int R = 64 / G;
   const int64_t row0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * (R * U);
   if (row0 >= a.n_rows) return;
-  int64_t wave_tok;
-  const int wave_at = rows_of_wave(a.c, a.q, row0, R * U, a.n_rows, lane, wave_tok);
   const bool is_k = blockIdx.z == 0;
   const int half = a.c.dh >> 1;
   const Rows& in = is_k ? a.k : a.v;
@@ -232,13 +251,24 @@ __global__ __launch_bounds__(256) void paged_write_kernel(const PagedWriteArgs a
   constexpr bool Q = ST == REFLEX_STORE_FP8 || ST == REFLEX_STORE_INT8;
   typedef typename std::conditional<Q, double, float>::type F;  // what a rotation is computed in
   const int h0 = blockIdx.y * a.heads_per, h1 = min(a.c.n_kv, h0 + a.heads_per);
+  // the next (row, head)'s values are always under way, the first ones while
+  // the rows' places are looked up
+  Raw8<T> nu, nw;
+  auto fetch = [&](int it, int h) __attribute__((always_inline)) {
+    const int64_t row = min(row0 + it * R + sub, a.n_rows - 1);
+    const T* x = reinterpret_cast<const T*>(in.p) + row * in.rs + h * in.hs + 8 * g;
+    nu.load(x);
+    nw.load(x + half);
+  };
+  fetch(0, h0);
+  int64_t wave_tok;
+  const int wave_at = rows_of_wave(a.c, a.q, row0, R * U, a.n_rows, lane, wave_tok);
 #pragma unroll 1
   for (int it = 0; it < U; ++it) {
     const int64_t row = row0 + it * R + sub;
     const int at = __shfl(wave_at, it * R + sub, 64);
     const int64_t tok = (int64_t)__shfl((long long)wave_tok, it * R + sub, 64);
     const bool live = at >= 0;
-    const T* x = reinterpret_cast<const T*>(in.p) + row * in.rs + 8 * g;
     F cs[8], sn[8];
     if (rot && live) {
       double f[8];
@@ -255,13 +285,10 @@ __global__ __launch_bounds__(256) void paged_write_kernel(const PagedWriteArgs a
     for (int h = h0; h < h1; ++h) {
       float u[8], w[8];
       const int64_t prow = (int64_t)at + ((int64_t)h << a.c.shift);
-      if (live) {
-        ld8(x + h * in.hs, u);
-        ld8(x + h * in.hs + half, w);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] = w[i] = 0.f;
-      }
+      nu.to_f(u);
+      nw.to_f(w);
+      if (h + 1 < h1) fetch(it, h + 1);
+      else if (it + 1 < U) fetch(it + 1, h0);
       auto put = [&](const auto* p, const auto* q) __attribute__((always_inline)) {
         uint32_t amax = 0;
 #pragma unroll

@@ -21,10 +21,10 @@ _STORES = {torch.float32: STORE_F32, torch.bfloat16: STORE_BF16, torch.float8_e4
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
 
-def _rows(x: torch.Tensor, heads: int, head_dim: int, device: torch.device, what: str) -> RowsC:
-    """The C view of [rows][heads][head_dim]; a dimension of one element may have any stride."""
-    if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != head_dim:
-        raise ValueError(f"{what} is [rows, {heads}, {head_dim}], got {tuple(x.shape)}")
+def _rows(x: torch.Tensor, n: int, heads: int, head_dim: int, device: torch.device, what: str) -> RowsC:
+    """The C view of [n][heads][head_dim]; a dimension of one element may have any stride."""
+    if x.shape != (n, heads, head_dim):
+        raise ValueError(f"{what} is [{n}, {heads}, {head_dim}], got {tuple(x.shape)}")
     if x.device != device:
         raise ValueError(f"{what} is on {x.device}, not on {device}")
     if x.requires_grad and torch.is_grad_enabled():
@@ -32,7 +32,7 @@ def _rows(x: torch.Tensor, heads: int, head_dim: int, device: torch.device, what
     rs, hs, es = x.stride()
     if es != 1:
         raise ValueError(f"{what} needs contiguous heads")
-    return RowsC(x.data_ptr(), rs if x.shape[0] > 1 else 0, hs if heads > 1 else 0)
+    return RowsC(x.data_ptr(), rs if n > 1 else 0, hs if heads > 1 else 0)
 
 
 def _dtype(t: torch.dtype) -> int:
@@ -43,23 +43,25 @@ def _dtype(t: torch.dtype) -> int:
 
 
 def _index(x: torch.Tensor, shape: Sequence[int], dtype: torch.dtype, what: str, device=None) -> int:
-    if x.dtype != dtype or tuple(x.shape) != tuple(shape) or not x.is_contiguous():
+    if x.dtype != dtype or x.shape != tuple(shape) or not x.is_contiguous():
         raise ValueError(f"{what} is a contiguous {dtype} tensor of shape {tuple(shape)}")
-    if x.device.type != "cuda" or (device is not None and x.device != device):
+    if not x.is_cuda or (device is not None and x.device != device):
         raise ValueError(f"{what} is on {x.device}, not on {device or 'a GPU'}")
     return x.data_ptr()
 
 
 def _call(device: torch.device, what: str, fn, *args) -> None:
     """fn(*args, stream) with the caller's current stream of `device`, that device current for the call."""
-    if device.type != "cuda":
+    idx = device.index
+    if device.type != "cuda" or idx is None:
         raise ValueError(f"{what} runs on a GPU, not on {device}")
-    idx = device.index if device.index is not None else torch.cuda.current_device()
     if idx == torch.cuda.current_device():
-        _check(fn(*args, _raw_stream(idx)), what)
+        status = fn(*args, _raw_stream(idx))
     else:
         with torch.cuda.device(idx):
-            _check(fn(*args, _raw_stream(idx)), what)
+            status = fn(*args, _raw_stream(idx))
+    if status:
+        _check(status, what)
 
 
 class Rotary:
@@ -92,15 +94,18 @@ class Rotary:
         if x.dim() != 3:
             raise ValueError(f"x is [rows, heads, head_dim], got {tuple(x.shape)}")
         n, heads, dh = x.shape
+        device = x.device
+        xr = _rows(x, n, heads, self.head_dim, device, "x")
         if out is None:
-            out = torch.empty((n, heads, dh), dtype=x.dtype, device=x.device)
-        elif out.dtype != x.dtype or out.shape[0] != n:
-            raise ValueError("out has x's rows and type")
-        xr = _rows(x, heads, self.head_dim, x.device, "x")
-        yr = _rows(out, heads, self.head_dim, x.device, "out")
-        p, ps = self._positions(positions, n, x.device)
+            out = torch.empty((n, heads, dh), dtype=x.dtype, device=device)
+            yr = RowsC(out.data_ptr(), heads * dh, dh)
+        else:
+            if out.dtype != x.dtype:
+                raise ValueError("out has x's type")
+            yr = _rows(out, n, heads, dh, device, "out")
+        p, ps = self._positions(positions, n, device)
         if heads:
-            _call(x.device, "reflex_rotary_apply", self.lib.reflex_rotary_apply, self._ref, p, ps, ctypes.byref(xr),
+            _call(device, "reflex_rotary_apply", self.lib.reflex_rotary_apply, self._ref, p, ps, ctypes.byref(xr),
                   ctypes.byref(yr), n, heads, _dtype(x.dtype), int(inverse))
         return out
 
@@ -166,11 +171,11 @@ class PagedCache:
         """Write the batch's rows k, v [rows, kv heads, head dim] into their pages, the keys rotated first where a
         plan is given: by ``positions``, or by each token's index in its sequence."""
         n = k.shape[0]
-        if v.shape != k.shape or v.dtype != k.dtype:
-            raise ValueError("k and v have one shape and type")
-        kr = _rows(k, self.n_kv_heads, self.head_dim, self.device, "k")
-        vr = _rows(v, self.n_kv_heads, self.head_dim, self.device, "v")
-        p, ps = (None, 0) if positions is None else (0, 0)
+        if v.dtype != k.dtype:
+            raise ValueError("k and v have one type")
+        kr = _rows(k, n, self.n_kv_heads, self.head_dim, self.device, "k")
+        vr = _rows(v, n, self.n_kv_heads, self.head_dim, self.device, "v")
+        p, ps = None, 0
         if positions is not None:
             if rotary is None:
                 raise ValueError("positions need a rotary plan")
@@ -186,10 +191,10 @@ class PagedCache:
             kv = torch.empty((2, n_rows, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device)
             out = (kv[0], kv[1])
         k, v = out
-        if k.shape != v.shape or k.dtype != v.dtype or k.shape[0] != n_rows:
-            raise ValueError("out is two tensors of n_rows rows and one type")
-        kr = _rows(k, self.n_kv_heads, self.head_dim, self.device, "k")
-        vr = _rows(v, self.n_kv_heads, self.head_dim, self.device, "v")
+        if k.dtype != v.dtype:
+            raise ValueError("out is two tensors of one type")
+        kr = _rows(k, n_rows, self.n_kv_heads, self.head_dim, self.device, "k")
+        vr = _rows(v, n_rows, self.n_kv_heads, self.head_dim, self.device, "v")
         _call(self.device, "reflex_paged_read", self.lib.reflex_paged_read, self._ref, self._batch(batch),
               ctypes.byref(kr), ctypes.byref(vr), n_rows, _dtype(k.dtype))
         return out
@@ -202,18 +207,21 @@ class PagedCache:
         stream."""
         if q.dim() != 3:
             raise ValueError(f"q is [rows, heads, head_dim], got {tuple(q.shape)}")
-        n, heads, _ = q.shape
+        n, heads, dh = q.shape
         dt = _dtype(q.dtype)
+        qr = _rows(q, n, heads, self.head_dim, self.device, "q")
         if out is None:
-            out = torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=q.device)
-        elif out.dtype != q.dtype or out.shape[0] != n:
-            raise ValueError("out has q's rows and type")
-        qr = _rows(q, heads, self.head_dim, self.device, "q")
-        yr = _rows(out, heads, self.head_dim, self.device, "out")
+            out = torch.empty((n, heads, dh), dtype=q.dtype, device=self.device)
+            yr = RowsC(out.data_ptr(), heads * dh, dh)
+        else:
+            if out.dtype != q.dtype:
+                raise ValueError("out has q's type")
+            yr = _rows(out, n, heads, dh, self.device, "out")
         ref = self._batch(batch)
         need = ctypes.c_size_t(0)
-        _check(self.lib.reflex_paged_attention_workspace(self._ref, ref, n, heads, dt, ctypes.byref(need)),
-               "reflex_paged_attention_workspace")
+        status = self.lib.reflex_paged_attention_workspace(self._ref, ref, n, heads, dt, ctypes.byref(need))
+        if status:
+            _check(status, "reflex_paged_attention_workspace")
         nb = need.value
         ws = torch.empty(nb, dtype=torch.uint8, device=self.device) if nb else None
         _call(self.device, "reflex_paged_attention", self.lib.reflex_paged_attention, self._ref, ref,
