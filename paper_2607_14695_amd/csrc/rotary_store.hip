@@ -24,13 +24,20 @@ RFX_DEV void st8(float* p, const float* v) {
   st16(p, f_to_frag(v, 0.f));
   st16(p + 4, f_to_frag(v + 4, 0.f));
 }
-RFX_DEV void st8(bf16_t* p, const float* v) { st16(p, f_to_frag(v, bf16_t(0))); }
+RFX_DEV uint32_t pack2(float a, float b) {  // to nearest even, NaN kept
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_v;
+  const bf16x2_v v = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+RFX_DEV void st8(bf16_t* p, const float* v) {
+  st16(p, make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])));
+}
 
 // Angle of a pair at a position, as a fraction of a turn in [-1/2, 1/2]: the
 // product and its reduction in 64 bits, so far positions keep 2^-53 of the
 // product (a position of 10^6 keeps the angle to 2e-10).
-RFX_DEV double turn_of(int64_t pos, double turns) {
-  const double t = (double)pos * turns;
+RFX_DEV double turn_of(double pos, double turns) {
+  const double t = pos * turns;
   return t - rint(t);
 }
 
@@ -39,15 +46,23 @@ RFX_DEV double turn_of(int64_t pos, double turns) {
 // once, and the pair's one is selected.
 RFX_DEV void turns_of(const reflex_rotary& plan, const int64_t* pos, int64_t ps, int64_t row, int64_t tok, int g,
                       double* f) {
-  int64_t p[REFLEX_MAX_AXES];
+  const double* const turns = plan.turns + 8 * g;
+  const double first = (double)(pos ? pos[row] : tok);
+  if (plan.n_axes == 1 || !pos) {
 #pragma unroll
-  for (int a = 0; a < REFLEX_MAX_AXES; ++a) p[a] = pos ? pos[(a < plan.n_axes ? a : 0) * ps + row] : tok;
+    for (int i = 0; i < 8; ++i) f[i] = turn_of(first, turns[i]);
+    return;
+  }
+  double p[REFLEX_MAX_AXES];
+  p[0] = first;
+#pragma unroll
+  for (int a = 1; a < REFLEX_MAX_AXES; ++a) p[a] = (double)pos[(a < plan.n_axes ? a : 0) * ps + row];
   const uint64_t axes = *reinterpret_cast<const uint64_t*>(plan.axis + 8 * g);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int a = (int)(axes >> (8 * i)) & 3;
-    const int64_t lo = a & 1 ? p[1] : p[0], hi = a & 1 ? p[3] : p[2];
-    f[i] = turn_of(a & 2 ? hi : lo, plan.turns[8 * g + i]);
+    const double lo = a & 1 ? p[1] : p[0], hi = a & 1 ? p[3] : p[2];
+    f[i] = turn_of(a & 2 ? hi : lo, turns[i]);
   }
 }
 
@@ -133,27 +148,6 @@ RFX_DEV void sincos_turn(double f, double* sn, double* cs) {
   *cs = (n + 1) & 2 ? -b : b;
 }
 
-// x / scale to the nearest integer, ties to even.  In 64 bits the product with
-// the reciprocal is within 2^-50 of the quotient, so only a quotient that close
-// to a border needs the division.
-RFX_DEV int code_int8(double x, double scale, double inv) {
-  const double t = x * inv;
-  double r = rint(t);
-  if (fabs(fabs(t - r) - 0.5) < 1e-9) r = rint(x / scale);
-  return max(-127, min(127, (int)r));
-}
-// In 32 bits the product is within 2^-15 of the quotient.
-RFX_DEV int code_int8(float x, float scale, float inv) {
-  const float t = x * inv;
-  float r = rintf(t);
-  if (fabsf(fabsf(t - r) - 0.5f) < 0x1p-14f) r = (float)rint((double)x / (double)scale);
-  return max(-127, min(127, (int)r));
-}
-
-// what the conversion to e4m3 rounds: x / scale exactly, or rounded to odd
-RFX_DEV float fp8_source(double x, double inv) { return odd_float(x * inv); }
-RFX_DEV float fp8_source(float x, float inv) { return x * inv; }
-
 // Scale of a row from the bits of its largest magnitude; NaN for a row with a
 // value that is not finite.
 template <int ST>
@@ -167,24 +161,38 @@ RFX_DEV float row_scale(uint32_t amax) {
   return __uint_as_float((uint32_t)(k + 127) << 23);
 }
 
-// The codes of 8 values as 8 bytes.  A rotated key comes in 64 bits (F =
-// double); other values are what they are in fp32.
+// The codes of 8 values as 8 bytes, from their fp32 form f and the values x
+// themselves (a rotated key comes in 64 bits).  No border between codes can lie
+// between x and f unless f is next to it: in int8 within 2^-14 of a half (the
+// product's error is under 2^-15), in fp8 on it (borders have five significant
+// bits).  Those few are decided from x.
 template <int ST, typename F>
-RFX_DEV uint2 codes8(const F* x, float scale) {
+RFX_DEV uint2 codes8(const float* f, const F* x, float scale) {
   uint32_t w[2] = {0, 0};
   if (!(scale < INFINITY)) return make_uint2(0u, 0u);
-  const F s = (F)scale, inv = F(1) / s;
+  const float inv = 1.f / scale;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     if (ST == REFLEX_STORE_INT8) {
+      int c[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w[i] |= (uint32_t)(code_int8(x[4 * i + j], s, inv) & 255) << (8 * j);
+      for (int j = 0; j < 4; ++j) {
+        const float t = f[4 * i + j] * inv;
+        float r = rintf(t);
+        if (fabsf(fabsf(t - r) - 0.5f) < 0x1p-14f) r = (float)rint((double)x[4 * i + j] / (double)scale);
+        c[j] = (int)r;  // -127 .. 127: f is at most the row's maximum
+      }
+      w[i] = (uint32_t)(c[0] & 255) | (uint32_t)(c[1] & 255) << 8 | (uint32_t)(c[2] & 255) << 16 | (uint32_t)c[3] << 24;
     } else {
-      float f[4];
+      float y[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) f[j] = fminf(fmaxf(fp8_source(x[4 * i + j], inv), -448.f), 448.f);  // inv: a power of two
-      int v = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
-      w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], v, true);
+      for (int j = 0; j < 4; ++j) {
+        y[j] = f[4 * i + j];
+        if (sizeof(F) == 8 && !(__float_as_uint(y[j]) & 0xffffu)) y[j] = odd_float((double)x[4 * i + j]);
+        y[j] *= inv;  // a power of two
+      }
+      int v = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+      w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], v, true);
     }
   }
   return make_uint2(w[0], w[1]);
@@ -233,14 +241,18 @@ template <> struct Raw8<bf16_t> {
   RFX_DEV void to_f(float* o) const { frag_to_f(a, o, bf16_t(0)); }
 };
 
-// blockIdx.z: 0 = K (rotated), 1 = V.  A wave takes U times 64 / G rows.
-template <typename T, int ST, int U>
+// blockIdx.z: 0 = K (rotated), 1 = V.  A wave takes 64 / G rows.  Bound by the
+// vector unit where keys are rotated for an 8-bit store: 32 frames of 768 keys
+// of 256 take 21 us with V, 8 us of them memory's.  (Measured slower: four times
+// the rows a wave, 22 us and, with eight 128-wide heads, 89 against 78 us; K and
+// V side by side in turn, 25 us.)
+template <typename T, int ST>
 __global__ __launch_bounds__(256) void paged_write_kernel(const PagedWriteArgs a) {
   const int G = a.c.dh >> 4;  // 4, 8 or 16
   const int lane = threadIdx.x & 63;
   const int g = lane & (G - 1), sub = lane / G;
   const int R = 64 / G;
-  const int64_t row0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * (R * U);
+  const int64_t row0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * R;
   if (row0 >= a.n_rows) return;
   const bool is_k = blockIdx.z == 0;
   const int half = a.c.dh >> 1;
@@ -251,83 +263,82 @@ __global__ __launch_bounds__(256) void paged_write_kernel(const PagedWriteArgs a
   constexpr bool Q = ST == REFLEX_STORE_FP8 || ST == REFLEX_STORE_INT8;
   typedef typename std::conditional<Q, double, float>::type F;  // what a rotation is computed in
   const int h0 = blockIdx.y * a.heads_per, h1 = min(a.c.n_kv, h0 + a.heads_per);
-  // the next (row, head)'s values are always under way, the first ones while
-  // the rows' places are looked up
+  // the next head's values are always under way, the first ones while the rows'
+  // places are looked up
   Raw8<T> nu, nw;
-  auto fetch = [&](int it, int h) __attribute__((always_inline)) {
-    const int64_t row = min(row0 + it * R + sub, a.n_rows - 1);
-    const T* x = reinterpret_cast<const T*>(in.p) + row * in.rs + h * in.hs + 8 * g;
-    nu.load(x);
-    nw.load(x + half);
+  const int64_t row = row0 + sub;
+  const T* const x = reinterpret_cast<const T*>(in.p) + min(row, a.n_rows - 1) * in.rs + 8 * g;
+  auto fetch = [&](int h) __attribute__((always_inline)) {
+    nu.load(x + h * in.hs);
+    nw.load(x + h * in.hs + half);
   };
-  fetch(0, h0);
+  fetch(h0);
   int64_t wave_tok;
-  const int wave_at = rows_of_wave(a.c, a.q, row0, R * U, a.n_rows, lane, wave_tok);
-#pragma unroll 1
-  for (int it = 0; it < U; ++it) {
-    const int64_t row = row0 + it * R + sub;
-    const int at = __shfl(wave_at, it * R + sub, 64);
-    const int64_t tok = (int64_t)__shfl((long long)wave_tok, it * R + sub, 64);
-    const bool live = at >= 0;
-    F cs[8], sn[8];
-    if (rot && live) {
-      double f[8];
-      turns_of(a.plan, a.pos, a.ps, row, tok, g, f);
+  const int wave_at = rows_of_wave(a.c, a.q, row0, R, a.n_rows, lane, wave_tok);
+  const int at = __shfl(wave_at, sub, 64);
+  const int64_t tok = (int64_t)__shfl((long long)wave_tok, sub, 64);
+  const bool live = at >= 0;
+  F cs[8], sn[8];
+  if (rot && live) {
+    double f[8];
+    turns_of(a.plan, a.pos, a.ps, row, tok, g, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (Q) sincos_turn(f[i], &sn[i], &cs[i]);
+      else sincospif(2.f * (float)f[i], &sn[i], &cs[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) cs[i] = sn[i] = F(0);
+  }
+  for (int h = h0; h < h1; ++h) {
+    float u[8], w[8];
+    const int64_t prow = (int64_t)at + ((int64_t)h << a.c.shift);
+    nu.to_f(u);
+    nw.to_f(w);
+    if (h + 1 < h1) fetch(h + 1);
+    auto put = [&](const auto* p, const auto* q) __attribute__((always_inline)) {
+      uint32_t amax = 0;
+      float fp[8], fq[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if constexpr (Q) sincos_turn(f[i], &sn[i], &cs[i]);
-        else sincospif(2.f * (float)f[i], &sn[i], &cs[i]);
+        fp[i] = (float)p[i];
+        fq[i] = (float)q[i];
+        amax = max(amax, max(__float_as_uint(fp[i]) & 0x7fffffffu, __float_as_uint(fq[i]) & 0x7fffffffu));
       }
-    } else {
+      for (int o = 1; o < G; o <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o, 64));
+      if (live) {
+        const float scale = row_scale<ST>(amax);
+        char* y = out + prow * a.c.dh + 8 * g;
+        *reinterpret_cast<uint2*>(y) = codes8<ST>(fp, p, scale);
+        *reinterpret_cast<uint2*>(y + half) = codes8<ST>(fq, q, scale);
+        if (g == 0) scales[prow] = scale;
+      }
+    };
+    if (rot) {
+      F p[8], q[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) cs[i] = sn[i] = F(0);
-    }
-    for (int h = h0; h < h1; ++h) {
-      float u[8], w[8];
-      const int64_t prow = (int64_t)at + ((int64_t)h << a.c.shift);
-      nu.to_f(u);
-      nw.to_f(w);
-      if (h + 1 < h1) fetch(it, h + 1);
-      else if (it + 1 < U) fetch(it + 1, h0);
-      auto put = [&](const auto* p, const auto* q) __attribute__((always_inline)) {
-        uint32_t amax = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          amax = max(amax, max(__float_as_uint((float)p[i]) & 0x7fffffffu, __float_as_uint((float)q[i]) & 0x7fffffffu));
-        for (int o = 1; o < G; o <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o, 64));
-        if (live) {
-          const float scale = row_scale<ST>(amax);
-          char* y = out + prow * a.c.dh + 8 * g;
-          *reinterpret_cast<uint2*>(y) = codes8<ST>(p, scale);
-          *reinterpret_cast<uint2*>(y + half) = codes8<ST>(q, scale);
-          if (g == 0) scales[prow] = scale;
-        }
-      };
-      if (rot) {
-        F p[8], q[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          p[i] = (F)u[i] * cs[i] - (F)w[i] * sn[i];
-          q[i] = (F)w[i] * cs[i] + (F)u[i] * sn[i];
-        }
-        if constexpr (Q) {
-          put(p, q);
-          continue;
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            u[i] = p[i];
-            w[i] = q[i];
-          }
-        }
+      for (int i = 0; i < 8; ++i) {
+        p[i] = (F)u[i] * cs[i] - (F)w[i] * sn[i];
+        q[i] = (F)w[i] * cs[i] + (F)u[i] * sn[i];
       }
       if constexpr (Q) {
-        put(u, w);
-      } else if (live) {
-        T* y = reinterpret_cast<T*>(out) + prow * a.c.dh + 8 * g;
-        st8(y, u);
-        st8(y + half, w);
+        put(p, q);
+        continue;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          u[i] = p[i];
+          w[i] = q[i];
+        }
       }
+    }
+    if constexpr (Q) {
+      put(u, w);
+    } else if (live) {
+      T* y = reinterpret_cast<T*>(out) + prow * a.c.dh + 8 * g;
+      st8(y, u);
+      st8(y + half, w);
     }
   }
 }
@@ -344,10 +355,11 @@ RFX_DEV void decode8(const uint2& c, float scale, float* o) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[4 * i + j] = (float)(int)(int8_t)(w[i] >> (8 * j)) * scale;
     } else {
-      o[4 * i] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 0) * scale;
-      o[4 * i + 1] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 1) * scale;
-      o[4 * i + 2] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 2) * scale;
-      o[4 * i + 3] = __builtin_amdgcn_cvt_f32_fp8((int)w[i], 3) * scale;
+      const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
+      o[4 * i] = a[0] * scale;
+      o[4 * i + 1] = a[1] * scale;
+      o[4 * i + 2] = b[0] * scale;
+      o[4 * i + 3] = b[1] * scale;
     }
   }
 }
@@ -430,8 +442,9 @@ hipError_t launch_rotary(const RotaryArgs& args, hipStream_t s) {
 template hipError_t launch_rotary<float>(const RotaryArgs&, hipStream_t);
 template hipError_t launch_rotary<bf16_t>(const RotaryArgs&, hipStream_t);
 
-// Rows of a wave, in units of 64 / G: four where that still fills the chip.
-int pick_unroll(int64_t threads) { return threads >= 4 * 256 * 1024 ? 4 : 1; }
+// Rows of a wave, in units of 64 / G: four where that leaves two waves to a
+// SIMD (looking up the rows' places is a third of a single unit's work).
+int pick_unroll(int64_t threads) { return threads >= 4 * 2 * 1024 * 64 ? 4 : 1; }
 
 template <typename T>
 hipError_t launch_paged_write(const PagedWriteArgs& args, int store, hipStream_t s) {
@@ -439,15 +452,11 @@ hipError_t launch_paged_write(const PagedWriteArgs& args, int store, hipStream_t
   const int G = a.c.dh >> 4;
   a.heads_per = pick_heads_per(2 * a.n_rows * G, a.c.n_kv);
   const unsigned heads = (a.c.n_kv + a.heads_per - 1) / a.heads_per;
-  const int U = pick_unroll(2 * a.n_rows * G * heads);
-  const int rows_per_block = 4 * (64 / G) * U;
-  const dim3 grid((unsigned)((a.n_rows + rows_per_block - 1) / rows_per_block), heads, 2);
+  const int rows_per_block = 4 * (64 / G);
+  const unsigned blocks = (unsigned)((a.n_rows + rows_per_block - 1) / rows_per_block);
+  const dim3 grid(blocks, heads, 2);
   auto go = [&](auto S) {
-    constexpr int ST = decltype(S)::value;
-    if (U == 4)
-      RFX_LAUNCH((paged_write_kernel<T, ST, 4>), grid, dim3(256), 0, s, a);
-    else
-      RFX_LAUNCH((paged_write_kernel<T, ST, 1>), grid, dim3(256), 0, s, a);
+    RFX_LAUNCH((paged_write_kernel<T, decltype(S)::value>), grid, dim3(256), 0, s, a);
   };
   if (store == REFLEX_STORE_FP8) go(std::integral_constant<int, REFLEX_STORE_FP8>{});
   else if (store == REFLEX_STORE_INT8) go(std::integral_constant<int, REFLEX_STORE_INT8>{});
