@@ -97,10 +97,23 @@ template <int N> RFX_DEV void wait_copies_if(bool newer) {
 // ---------------------------------------------------------------------------
 // shared pieces of the tiled kernels
 // ---------------------------------------------------------------------------
-// lds_dma16 from a wave-uniform base, with an offset added to both addresses
-template <int OFF> RFX_DEV void lds_dma16_at(const void* base, uint32_t off, void* lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3"
-               :: "v"(off), "s"(base), "s"((unsigned)(size_t)lds), "n"(OFF) : "memory");
+// N copies as lds_dma16's from a wave-uniform base, each 1 KB further than the
+// one before on both sides: one run of bytes
+template <int N> RFX_DEV void lds_dma16_run(const void* base, const uint32_t (&off)[N], void* lds) {
+  static_assert(N == 1 || N == 2 || N == 4, "up to four copies");
+  const unsigned m0 = (unsigned)(size_t)lds;
+  if constexpr (N == 1) {
+    lds_dma16(base, off[0], lds);
+  } else if constexpr (N == 2) {
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %2\n\t"
+                 "global_load_lds_dwordx4 %1, %2 offset:1024"
+                 :: "v"(off[0]), "v"(off[1]), "s"(base), "s"(m0) : "memory");
+  } else {
+    asm volatile("s_mov_b32 m0, %5\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %4\n\t"
+                 "global_load_lds_dwordx4 %1, %4 offset:1024\n\tglobal_load_lds_dwordx4 %2, %4 offset:2048\n\t"
+                 "global_load_lds_dwordx4 %3, %4 offset:3072"
+                 :: "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base), "s"(m0) : "memory");
+  }
 }
 
 template <int N, typename F> RFX_DEV void static_for(F&& f) {
@@ -797,12 +810,17 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
     auto run_of = [&](const char* base, int rr) __attribute__((always_inline)) {
       return base + ((int64_t)__builtin_amdgcn_readlane(rr, wave * (KT / 4)) + hoff) * RB;
     };
-    auto copy_one = [&](const char* run, auto sw, const uint32_t (&off)[NO], unsigned char* dst, auto J)
+    // NB copies from the B-th group on
+    constexpr int NB = NI < 4 ? NI : 4;
+    auto copy_some = [&](const char* run, auto sw, const uint32_t (&off)[NO], unsigned char* dst, auto B)
         __attribute__((always_inline)) {
-      constexpr int j = decltype(J)::value;
-      // (copies four apart: the swizzle's bits beyond those of four copies)
-      const uint32_t o = j < 4 ? off[j % NO] : off[j % NO] ^ ((sw(j * RPC) ^ sw(j % 4 * RPC)) << 4);
-      lds_dma16_at<(j & 3) * 1024>(run + (j >> 2) * 4096, o, dst + wave * NI * 1024 + (j >> 2) * 4096);
+      constexpr int b = decltype(B)::value;
+      // (beyond the first four copies the swizzle differs by the bits above theirs)
+      const uint32_t x = b ? (sw(4 * b * RPC) ^ sw(0)) << 4 : 0;
+      uint32_t o[NB];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) o[j] = off[j] ^ x;
+      lds_dma16_run<NB>(run + b * 4096, o, dst + wave * NI * 1024 + b * 4096);
     };
     auto copy_any = [&](const char* base, auto sw, int rr, unsigned char* dst) __attribute__((always_inline)) {
 #pragma unroll 4
@@ -996,12 +1014,12 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
         for (int q = 0; q < 16; ++q)
           if (g == T2 / 16 + q * 11 * T2 / 128) pair(x, whole, q, cur, pw);
         // copies over the first three quarters
-        constexpr int STEP = 3 * T2 / 2 / (2 * NI);
-        if constexpr (g % STEP == STEP - 1 && g / STEP < 2 * NI) {
+        constexpr int NG = 2 * NI / NB, STEP = 3 * T2 / 2 / NG;
+        if constexpr (g % STEP == STEP / 2 && g / STEP < NG) {
           constexpr int c = g / STEP;
           if (easy) {
-            if constexpr (c < NI) copy_one(run_k, swk, koff, dk, std::integral_constant<int, c>{});
-            else copy_one(run_v, swv, voff, dv, std::integral_constant<int, c - NI>{});
+            if constexpr (c < NG / 2) copy_some(run_k, swk, koff, dk, std::integral_constant<int, c>{});
+            else copy_some(run_v, swv, voff, dv, std::integral_constant<int, c - NG / 2>{});
           }
         }
       };
