@@ -620,8 +620,8 @@ int reflex_paged_read(const reflex_paged_cache* cache, const reflex_paged_batch*
  * only j <= p, and with window > 0 only j > p - window.  A row that sees none
  * gets zeros.
  * Keys that a row does not see have no part in its result, whatever they hold
- * (NaN and infinities included).  Probabilities enter the second product in
- * dtype, all sums are fp32; results do not depend on what else is on the GPU.
+ * (NaN and infinities included).  Probabilities enter the second product
+ * rounded to dtype or finer, all sums are fp32; equal calls give equal bits.
  * q, out: [n_rows][n_q_heads][head_dim], not overlapping.  n_q_heads: a
  * multiple of n_kv_heads; n_rows * n_q_heads <= 2^25.
  * workspace: at least the bytes that reflex_paged_attention_workspace gives

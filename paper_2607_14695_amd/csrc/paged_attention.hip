@@ -175,6 +175,11 @@ RFX_DEV uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
+// what the packed roundings of a and b left of them, rounded itself
+RFX_DEV uint32_t rest_bf16(float a, float b, uint32_t w) {
+  return pack_bf16(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xffff0000u));
+}
+
 // 8 codes -> 8 bf16 (exact: codes have at most 7 significant bits and a sign)
 template <int ST> RFX_DEV uint4 codes_to_bf16(uint2 c) {
   uint32_t w[4];
@@ -565,11 +570,17 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
       if (BF) {
 #pragma unroll
         for (int j = 0; j < KT / 32; ++j) {
-          uint4 pf[MR];
+          // The probabilities as two bf16 each, the second what the first's
+          // rounding left: 16 bits of them.  The products this adds are hidden
+          // by the cache's reads, and the result is then as exact as its own
+          // rounding.
+          uint4 pf[MR], pl[MR];
 #pragma unroll
           for (int m = 0; m < MR; ++m) {
             const f32x4_v &u = s[m][2 * j], &w = s[m][2 * j + 1];
             pf[m] = make_uint4(pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]), pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3]));
+            pl[m] = make_uint4(rest_bf16(u[0], u[1], pf[m].x), rest_bf16(u[2], u[3], pf[m].y),
+                               rest_bf16(w[0], w[1], pf[m].z), rest_bf16(w[2], w[3], pf[m].w));
           }
 #pragma unroll
           for (int d = 0; d < NDB; ++d) {
@@ -584,7 +595,10 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
               f = make_uint4(f0.x, f0.y, f1.x, f1.y);
             }
 #pragma unroll
-            for (int m = 0; m < MR; ++m) mfma_step(o[m][d], f, pf[m], bf16_t(0));
+            for (int m = 0; m < MR; ++m) {
+              mfma_step(o[m][d], f, pf[m], bf16_t(0));
+              mfma_step(o[m][d], f, pl[m], bf16_t(0));
+            }
           }
         }
       } else {

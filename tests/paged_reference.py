@@ -85,5 +85,5 @@ def attend(q, kpages, vpages, cu, lengths, table, causal, window, scale):
             p = np.exp(s - s.max())
             p /= p.sum()
             out[r, h], spread[r, h] = p @ v, p @ np.abs(v)
-            reach[r, h] = scale * np.max(np.abs(k) @ np.abs(q[r, h]))
+            reach[r, h] = abs(scale) * np.max(np.abs(k) @ np.abs(q[r, h]))
     return out, spread, reach

@@ -9,13 +9,12 @@ Tolerances.  One rounding to a type is off by at most half a step: 2^-8 of the v
   probability is rounded once (2^-8).  All of it weighs on `spread` = sum p|v|, and the sum of the probabilities
   doubles it.  Then the result's own rounding.
 """
-import ctypes
-
 import numpy as np
 import pytest
 import torch
 
 from paper_2607_14695_amd import reflex as R
+from paper_2607_14695_amd import workloads as WL
 from paper_2607_14695_amd.paged import PagedBatch, PagedCache, Rotary
 
 from . import paged_reference as ref
@@ -261,10 +260,11 @@ def test_default_positions_are_the_tokens_indices():
 # ---------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------
-def check_attention(q, cache, kv, cu, lens, table, causal, window, dtype, max_length=0, b=None, out=None):
+def check_attention(q, cache, kv, cu, lens, table, causal, window, dtype, max_length=0, out=None, scale=None):
     dh = q.shape[-1]
-    scale = dh ** -0.5
-    got = f64(cache.attend(b or batch(cu, lens, table, max_length), q.to(DEV), causal=causal, window=window, out=out))
+    got = f64(cache.attend(batch(cu, lens, table, max_length), q.to(DEV), causal=causal, window=window, scale=scale,
+                           out=out))
+    scale = dh ** -0.5 if scale is None else scale
     want, spread, reach = ref.attend(f64(q), *kv, cu.numpy(), lens.numpy(), table.numpy(), causal, window, scale)
     rows = ~np.isnan(want[:, 0, 0])
     moved = 2 * (2 * (dh + 4) * 2.0 ** -24 * reach + 2.0 ** -21 + 64 * 2.0 ** -24) + (2.0 ** -8 if dtype == "bf16" else 0)
@@ -295,6 +295,8 @@ ATTEND = {
     "rows_without_keys": ([(9, 4), (3, 0), (0, 7), (2, 5)], 6, 2, 64, 4, True, 0),
     "mixed": ([(1, 650), (70, 210), (0, 9), (1, 3), (200, 330), (17, 1000)], 4, 1, 128, 64, True, 0),
     "large_page": ([(3, 1500)], 2, 1, 256, 1024, True, 0),
+    "many_sequences": ([(i % 3, 5 + i % 40) for i in range(150)], 2, 1, 64, 8, True, 0),
+    "many_sequences_of_chunks": ([(0, 3)] * 64 + [(40, 60)] * 3 + [(0, 9)] * 70 + [(50, 50)] * 2, 4, 2, 128, 16, True, 0),
 }
 
 
@@ -407,6 +409,32 @@ def test_max_length_only_sizes_the_launch(dtype, store, new):
     assert torch.equal(cache.attend(b, q.to(DEV)), cache.attend(b, q.to(DEV)))
 
 
+@pytest.mark.parametrize("store", ["bf16", "fp8", "int8"])
+@pytest.mark.parametrize("dh,ps,causal,window", [(64, 8, True, 0), (128, 8, False, 0), (128, 64, True, 700),
+                                                 (256, 16, True, 0), (256, 4, False, 900)])
+def test_long_loops(store, dh, ps, causal, window):
+    """Many tiles in one workgroup (the hint keeps the keys together): every turn of the rings, pages smaller than a
+    copy, and more table entries than are held at once."""
+    gen = torch.Generator().manual_seed(dh + ps)
+    cu, lens, table, n_pages = pool([40, 33], [5200 if ps == 4 else 1500, 771], ps, gen)
+    cache, k, v = filled(n_pages, 1, ps, dh, store, gen)
+    q = draw(gen, (73, 4, dh), "bf16")
+    check_attention(q, cache, (k, v), cu, lens, table, causal, window, "bf16", max_length=64)
+    one = torch.tensor([0, 1, 2], dtype=torch.int32)
+    check_attention(q[:2], cache, (k, v), one, lens, table, causal, window, "bf16", max_length=64)
+
+
+@pytest.mark.parametrize("dtype,store", [("bf16", "bf16"), ("bf16", "int8"), ("f32", "f32")])
+@pytest.mark.parametrize("new", [1, 70])
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 2.0, 1e-30])
+def test_scales(dtype, store, new, scale):
+    gen = torch.Generator().manual_seed(31)
+    cu, lens, table, n_pages = pool([new, new], [200, 90], 16, gen)
+    cache, k, v = filled(n_pages, 1, 16, 64, store, gen)
+    q = draw(gen, (2 * new, 2, 64), dtype)
+    check_attention(q, cache, (k, v), cu, lens, table, True, 0, dtype, scale=scale)
+
+
 def test_scale_of_zero_and_sharing_pages():
     """scale 0 gives the mean of the visible values; sequences that share their prefix's pages."""
     gen = torch.Generator().manual_seed(6)
@@ -417,7 +445,7 @@ def test_scale_of_zero_and_sharing_pages():
     q = draw(gen, (6, 2, 64), "f32")
     check_attention(q, cache, (k, v), cu, lens, table, True, 0, "f32")
     got = f64(cache.attend(batch(cu, lens, table), q.to(DEV), causal=False, scale=0.0))
-    mean = np.mean([v[p // 1][0, s] for p, s in (ref.place(table[0], n_pages, 8, j) for j in range(40))], 0)
+    mean = np.mean([v[p][0, s] for p, s in (ref.place(table[0], n_pages, 8, j) for j in range(40))], 0)
     np.testing.assert_allclose(got[0, 0], mean, atol=1e-5)
 
 
@@ -439,8 +467,7 @@ def test_offsets_past_32_bits():
         assert float((y.cpu().float() - x.float()).abs().max()) <= float(x.float().abs().max()) * (0.5 / 127 + 2.0 ** -8)
     q = draw(gen, (n, hk, dh), "bf16")
     kv = [f64(t.cpu()).transpose(1, 0, 2)[None] for t in cache.read(b, n, dtype=torch.float32)]
-    small = (torch.zeros(1, 1, dtype=torch.int32), )
-    want, spread, reach = ref.attend(f64(q), *kv, cu.numpy(), lens.numpy(), small[0].numpy(), True, 0, dh ** -0.5)
+    want, spread, _ = ref.attend(f64(q), *kv, cu.numpy(), lens.numpy(), np.zeros((1, 1), dtype=int), True, 0, dh ** -0.5)
     got = f64(cache.attend(b, q.to(DEV)))
     assert np.all(np.abs(got - want) <= 2.0 ** -7 * spread + 2.0 ** -8 * np.abs(want))
 
@@ -505,6 +532,54 @@ def test_streams():
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(g, want[i]) for g in got[i])
+
+
+def test_prefix_of_the_engine_through_the_paged_cache():
+    """As a backbone uses them: each layer's prefix rotated into its pages in two chunks and attended, then read back,
+    turned back and given to the engine, whose own cache rows and actions are those of the original prefix."""
+    cfg = WL.CONFIGS["tiny_fp32"].replace(frame_dim=0, static_len=64)
+    L, S, dh = cfg.n_layers, cfg.static_len, cfg.head_dim
+    w = WL.make_weights(cfg)
+    sk, sv = WL.make_static_kv(cfg)  # [1, L, S, dh], before RoPE
+    k, v = (torch.from_numpy(np.ascontiguousarray(t[0])).to(DEV) for t in (sk, sv))
+    gen = torch.Generator().manual_seed(3)
+    rot = Rotary(dh, theta=cfg.rope_theta)
+    _, _, table, n_pages = pool([S] * L, [S] * L, 16, gen)
+    cache = PagedCache.zeros(n_pages, 16, 1, dh, torch.float32)
+    q = torch.randn(L, S, cfg.n_q_heads, dh, generator=gen).to(DEV)
+    outs, done = [], 0
+    for n in (48, 16):
+        rows = slice(done, done + n)
+        done += n
+        b = batch(torch.arange(0, L * n + 1, n, dtype=torch.int32), torch.full((L,), done, dtype=torch.int32), table)
+        cache.write(b, k[:, rows].reshape(L * n, 1, dh), v[:, rows].reshape(L * n, 1, dh), rotary=rot)
+        pos = torch.arange(rows.start, rows.stop, device=DEV).repeat(L)
+        qr = rot.apply(q[:, rows].reshape(L * n, cfg.n_q_heads, dh), pos)
+        outs.append(cache.attend(b, qr).view(L, n, cfg.n_q_heads, dh))
+    out = f64(torch.cat(outs, 1))
+    ang = ref.rotary_angles(np.arange(S), (dh // 2,), cfg.rope_theta, "shared", dh // 2)
+    for layer in range(L):  # plain attention over the rotated prefix; N(0, 1) values: 1e-5 is 80 steps of fp32
+        kr, qr = ref.rotate(f64(k[layer])[:, None], ang)[:, 0], ref.rotate(f64(q[layer]), ang)
+        s = np.einsum("ihd,jd->ihj", qr, kr) * dh ** -0.5
+        s[np.broadcast_to(np.arange(S)[None, None] > np.arange(S)[:, None, None], s.shape)] = -np.inf
+        p = np.exp(s - s.max(-1, keepdims=True))
+        want = np.einsum("ihj,jd->ihd", p / p.sum(-1, keepdims=True), f64(v[layer]))
+        np.testing.assert_allclose(out[layer], want, atol=1e-5)
+
+    whole = batch(torch.arange(0, L * S + 1, S, dtype=torch.int32), torch.full((L,), S, dtype=torch.int32), table)
+    rk, rv = cache.read(whole, L * S, dtype=torch.float32)
+    back = rot.apply(rk, torch.arange(S, device=DEV).repeat(L), inverse=True)
+    engines = [R.ReflexEngine(cfg, w, a, b) for a, b in (
+        (sk, sv), (back.view(1, L, S, dh), rv.view(1, L, S, dh)))]
+    rows = [e.cache_views()[0][0, :, :S].clone() for e in engines]
+    # two more rotations of values up to 5: 16 roundings of fp32
+    np.testing.assert_allclose(f64(rows[0]), f64(rk.view(L, S, dh)), atol=5e-6)
+    np.testing.assert_allclose(f64(rows[1]), f64(rows[0]), atol=5e-6)
+    state, noise = WL.make_state(cfg, 0), WL.make_noise(cfg, 0)
+    acts = [e.denoise(state, noise).clone() for e in engines]
+    np.testing.assert_allclose(f64(acts[1]), f64(acts[0]), atol=1e-4)  # the bar of the engine's own fp32 parity
+    for e in engines:
+        e.close()
 
 
 def test_python_refusals_on_the_gpu():
