@@ -379,6 +379,30 @@ def test_what_is_not_seen_does_not_matter(dtype, dh, new, length, window):
         assert bool(torch.isposinf(got[-1, :, 3]).all() and got[-1, :, 4].isnan().all() and got[-1, :, 5:].isfinite().all())
 
 
+@pytest.mark.parametrize("dtype,store", [("bf16", "fp8"), ("bf16", "int8"), ("f32", "fp8")])
+@pytest.mark.parametrize("dh", [64, 128, 256])
+@pytest.mark.parametrize("new,length,window", [(1, 40, 0), (70, 400, 0), (200, 700, 64)])
+def test_scales_that_are_not_seen_do_not_matter(dtype, store, dh, new, length, window):
+    """NaN scales in every slot that no row sees, and for the last token, which only its own row does."""
+    gen = torch.Generator().manual_seed(19)
+    cu, lens, table, n_pages = pool([new], [length], 16, gen)
+    cache, k, v = filled(n_pages, 1, 16, dh, store, gen)
+    hide = torch.ones(n_pages, 16, dtype=torch.bool)
+    for j in range(max(0, length - new - window + 1) if window else 0, length):
+        hide[ref.place(table[0], n_pages, 16, j)] = False
+    q = draw(gen, (new, 2, dh), dtype)
+    for t in (cache.k_scale, cache.v_scale):
+        t[:, 0][hide.to(DEV)] = float("nan")
+    clean = check_attention(q, cache, (k, v), cu, lens, table, True, window, dtype)
+    if new > 1:
+        at = ref.place(table[0], n_pages, 16, length - 1)
+        for t in (cache.k_scale, cache.v_scale):
+            t[at[0], 0, at[1]] = float("nan")
+            got = f64(cache.attend(batch(cu, lens, table), q.to(DEV), window=window))
+            assert np.isnan(got[-1]).all()
+            np.testing.assert_array_equal(got[:-1], clean[:-1])
+
+
 @pytest.mark.parametrize("dtype,store", [("bf16", "bf16"), ("bf16", "int8"), ("f32", "f32")])
 def test_large_scores_and_queries_that_are_not_finite(dtype, store):
     """Scores far apart (one key takes all) and running maxima that move; a NaN query keeps to its row."""
