@@ -567,8 +567,8 @@ typedef struct reflex_paged_cache {
  * lengths[b] tokens, the last n_b = cu_rows[b+1] - cu_rows[b] of which are the
  * call's rows cu_rows[b] .. cu_rows[b+1] - 1, oldest first.  Token p of the
  * sequence lies in slot p % page_size of page page_table[b][p / page_size].
- * Rows outside [cu_rows[0], cu_rows[n_seqs]) belong to no sequence: they are
- * not read, and what an output holds there stays.
+ * Rows outside [cu_rows[0], cu_rows[n_seqs]) belong to no sequence: they have
+ * no part in the call, and what an output holds there stays.
  * A table entry outside [0, n_pages), and every token beyond max_pages pages
  * or before the sequence's start, is absent: nothing is written for it, it
  * reads as zeros and no query sees it.  Sequences may share pages that a call
@@ -623,7 +623,7 @@ int reflex_paged_read(const reflex_paged_cache* cache, const reflex_paged_batch*
  * (NaN and infinities included).  Probabilities enter the second product
  * rounded to dtype or finer, all sums are fp32; equal calls give equal bits.
  * q, out: [n_rows][n_q_heads][head_dim], not overlapping.  n_q_heads: a
- * multiple of n_kv_heads; n_rows * n_q_heads <= 2^25.
+ * multiple of n_kv_heads; n_rows * n_q_heads <= 2^23.
  * workspace: at least the bytes that reflex_paged_attention_workspace gives
  * (which may be 0), 256-byte aligned; private to the call until its work is
  * done.

@@ -205,7 +205,7 @@ int reflex_paged_attention_workspace(const reflex_paged_cache* cache, const refl
   RFX_CHECK(check_dtype(dtype));
   RFX_CHECK(check_batch(batch, cache, n_rows));
   RFX_CHECK(check_store(cache, dtype));
-  if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads || n_rows * (int64_t)n_q_heads > (int64_t(1) << 25))
+  if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads || n_rows * (int64_t)n_q_heads > (int64_t(1) << 23))
     return REFLEX_EINVAL;
   *bytes = n_rows == 0 || batch->n_seqs == 0 ? 0 : paged_attention_plan(*cache, *batch, n_rows, n_q_heads, dtype).bytes;
   return REFLEX_OK;
