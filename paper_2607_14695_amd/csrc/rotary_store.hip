@@ -58,11 +58,17 @@ RFX_DEV void turns_of(const reflex_rotary& plan, const int64_t* pos, int64_t ps,
 #pragma unroll
   for (int a = 1; a < REFLEX_MAX_AXES; ++a) p[a] = (double)pos[(a < plan.n_axes ? a : 0) * ps + row];
   const uint64_t axes = *reinterpret_cast<const uint64_t*>(plan.axis + 8 * g);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int a = (int)(axes >> (8 * i)) & 3;
+  auto of = [&](int a) __attribute__((always_inline)) {
     const double lo = a & 1 ? p[1] : p[0], hi = a & 1 ? p[3] : p[2];
-    f[i] = turn_of(a & 2 ? hi : lo, turns[i]);
+    return a & 2 ? hi : lo;
+  };
+  if (axes == (axes & 255) * 0x0101010101010101ull) {  // sections of whole eights
+    const double q = of((int)axes & 3);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = turn_of(q, turns[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = turn_of(of((int)(axes >> (8 * i)) & 3), turns[i]);
   }
 }
 
@@ -118,9 +124,9 @@ RFX_DEV float odd_float(double x) {
   return f;
 }
 
-// Sine and cosine of a fraction of a turn in [-1/2, 1/2], to a few 2^-53: the
-// nearest quarter turn is taken off, and the series of both functions (sine to
-// x^15, cosine to x^16) holds the rest, |x| <= pi / 4, to 2^-54 of 1.
+// Sine and cosine of a fraction of a turn in [-1/2, 1/2]: the
+// nearest quarter turn is taken off, and the Taylor series of both functions
+// (sine to x^15, cosine to x^14) hold the rest, |x| <= pi / 4, to 2^-49 of 1.
 RFX_DEV void sincos_turn(double f, double* sn, double* cs) {
   const double q = rint(4.0 * f);
   const double x = fma(q, -0.25, f) * 6.283185307179586477;
@@ -133,8 +139,7 @@ RFX_DEV void sincos_turn(double f, double* sn, double* cs) {
   s = fma(s, z, 1.0 / 120.0);
   s = fma(s, z, -1.0 / 6.0);
   s = fma(s * z, x, x);
-  double c = 1.0 / 20922789888000.0;
-  c = fma(c, z, -1.0 / 87178291200.0);
+  double c = -1.0 / 87178291200.0;
   c = fma(c, z, 1.0 / 479001600.0);
   c = fma(c, z, -1.0 / 3628800.0);
   c = fma(c, z, 1.0 / 40320.0);
@@ -144,8 +149,11 @@ RFX_DEV void sincos_turn(double f, double* sn, double* cs) {
   c = fma(c, z, 1.0);
   const int n = (int)q;  // -2 .. 2
   const double a = n & 1 ? c : s, b = n & 1 ? s : c;
-  *sn = n & 2 ? -a : a;
-  *cs = (n + 1) & 2 ? -b : b;
+  auto flip = [](double v, int by) __attribute__((always_inline)) {  // bit 1 of `by` on the sign
+    return __hiloint2double(__double2hiint(v) ^ ((by & 2) << 30), __double2loint(v));
+  };
+  *sn = flip(a, n);
+  *cs = flip(b, n + 1);
 }
 
 // Scale of a row from the bits of its largest magnitude; NaN for a row with a
