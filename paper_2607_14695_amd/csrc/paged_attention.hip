@@ -454,29 +454,53 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
       // S^T: block kb holds keys 16 kb + 4 g + i of query row c16
       f32x4_v s[MR][NKB];
 #pragma unroll
-      for (int b = 0; b < NKB; ++b) {
+      for (int b = 0; b < NKB; ++b)
 #pragma unroll
         for (int m = 0; m < MR; ++m) s[m][b] = f32x4_v{0.f, 0.f, 0.f, 0.f};
+      auto k_read = [&](int b, int k) __attribute__((always_inline)) {
         const int row = 16 * b + c16;
-        const unsigned char* kr = kb + row * RB;
-        if (!Q8) {
+        return ld16(kb + row * RB + (((4 * k + g) ^ swz(row)) << 4));
+      };
+      constexpr int NR = Q8 ? DH / 64 : NKS;  // reads of a row
+      if constexpr (BF) {
 #pragma unroll
-          for (int k = 0; k < NKS; ++k) {
-            const uint4 f = ld16(kr + (((4 * k + g) ^ swz(row)) << 4));
+        for (int b = 0; b < NKB; ++b)
 #pragma unroll
-            for (int m = 0; m < MR; ++m) mfma_step(s[m][b], f, qf[m][k], T(0));
-          }
-        } else {
+          for (int k = 0; k < NR; ++k) {
+            const uint4 c = k_read(b, k);
+            if (!Q8) {
 #pragma unroll
-          for (int k = 0; k < DH / 64; ++k) {
-            const uint4 c = ld16(kr + (((4 * k + g) ^ swz(row)) << 4));
-            if (BF) {
+              for (int m = 0; m < MR; ++m) mfma_step(s[m][b], c, qf[m][k], T(0));
+            } else {
               const uint4 f0 = codes_to_bf16<ST>(make_uint2(c.x, c.y)), f1 = codes_to_bf16<ST>(make_uint2(c.z, c.w));
 #pragma unroll
               for (int m = 0; m < MR; ++m) {
                 mfma_step(s[m][b], f0, qf[m][2 * k], T(0));
                 mfma_step(s[m][b], f1, qf[m][2 * k + 1], T(0));
               }
+            }
+          }
+      } else {
+        // fp32 is bound by its products: the next group of reads is under way
+        // while one is multiplied
+        constexpr int RG = Q8 ? 1 : 4, NG = NKB * NR / RG;
+        uint4 kf[2][RG];
+        auto request = [&](int n) __attribute__((always_inline)) {
+#pragma unroll
+          for (int i = 0; i < RG; ++i) kf[n & 1][i] = k_read((n * RG + i) / NR, (n * RG + i) % NR);
+        };
+        request(0);
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+          if (n + 1 < NG) request(n + 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int i = 0; i < RG; ++i) {
+            const int b = (n * RG + i) / NR, k = (n * RG + i) % NR;
+            const uint4 c = kf[n & 1][i];
+            if (!Q8) {
+#pragma unroll
+              for (int m = 0; m < MR; ++m) mfma_step(s[m][b], c, qf[m][k], T(0));
             } else {
               const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
@@ -487,6 +511,7 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
               }
             }
           }
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
       float4 ks[NKB];
@@ -588,27 +613,39 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
           }
         }
       } else {
+        // element (row 16 b + 4 g + e, column 16 d + c16): the swizzle of a row
+        // does not depend on b, and is an XOR
+        constexpr int SH = Q8 ? 4 : 6;  // 16 columns are one chunk of codes, four of fp32
+        uint32_t base[4], vf[2][4];
 #pragma unroll
-        for (int b = 0; b < NKB; ++b)
+        for (int e = 0; e < 4; ++e) {
+          const int row = 4 * g + e;
+          base[e] = row * RB + (Q8 ? (swz(row) << 4) + c16 : (((c16 >> 2) ^ swz(row)) << 4) + (c16 & 3) * 4);
+        }
+        auto request = [&](int n) __attribute__((always_inline)) {
 #pragma unroll
-          for (int d = 0; d < NDB; ++d) {
-            float f[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int row = 16 * b + 4 * g + e, col = 16 * d + c16;
-              if (Q8) {
-                f[e] = code_to_f32<ST>(vb[row * RB + (((col >> 4) ^ swz(row)) << 4) + (col & 15)]);
-              } else {
-                f[e] = *reinterpret_cast<const float*>(vb + row * RB + (((col >> 2) ^ swz(row)) << 4) + (col & 3) * 4);
-              }
-            }
-            const uint4 vf = f_to_frag(f, 0.f);
-#pragma unroll
-            for (int m = 0; m < MR; ++m) {
-              const float p[4] = {s[m][b][0], s[m][b][1], s[m][b][2], s[m][b][3]};
-              mfma_step(o[m][d], vf, f_to_frag(p, 0.f), 0.f);
-            }
+          for (int e = 0; e < 4; ++e) {
+            const unsigned char* at = vb + (base[e] ^ (n % NDB << SH)) + 16 * (n / NDB) * RB;
+            vf[n & 1][e] = Q8 ? (uint32_t)*at : *reinterpret_cast<const uint32_t*>(at);
           }
+        };
+        request(0);
+#pragma unroll
+        for (int n = 0; n < NKB * NDB; ++n) {
+          if (n + 1 < NKB * NDB) request(n + 1);
+          __builtin_amdgcn_sched_barrier(0);
+          const int b = n / NDB, d = n % NDB;
+          float f[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f[e] = Q8 ? code_to_f32<ST>(vf[n & 1][e]) : __uint_as_float(vf[n & 1][e]);
+          const uint4 v = f_to_frag(f, 0.f);
+#pragma unroll
+          for (int m = 0; m < MR; ++m) {
+            const float p[4] = {s[m][b][0], s[m][b][1], s[m][b][2], s[m][b][3]};
+            mfma_step(o[m][d], v, f_to_frag(p, 0.f), 0.f);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
       wait_lds();
       if (more) copy(pv, psv, r_next, easy, vb, vsc);
