@@ -20,6 +20,10 @@ namespace {
 // nothing has exp2(-infinity - m) = 0 and not NaN.
 constexpr float kFloor = -3.0e38f;
 
+// The running maximum of a row is raised only when a score exceeds it by 2^8:
+// probabilities then stay below 2^8, and the output is rescaled in few tiles.
+constexpr float kSlack = 8.f;
+
 // what a copy into LDS reads in place of a row that is not there
 __device__ const uint4 kZeros[1] = {};
 
@@ -543,21 +547,25 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
             top = fmaxf(top, v);
           }
         }
-        top = fmaxf(mx[m], across_rows(top, max2));
-        const float scale = __builtin_amdgcn_exp2f(mx[m] - top);
-        mx[m] = top;
+        top = across_rows(top, max2);
+        if (__ballot(top > mx[m] + kSlack)) {
+          const float nm = top > mx[m] + kSlack ? top : mx[m];
+          const float f = __builtin_amdgcn_exp2f(mx[m] - nm);
+          mx[m] = nm;
+          sum[m] *= f;
+#pragma unroll
+          for (int d = 0; d < NDB; ++d) o[m][d] *= f;
+        }
         float add = 0.f;
 #pragma unroll
         for (int b = 0; b < NKB; ++b)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float p = __builtin_amdgcn_exp2f(s[m][b][i] - top);
+            const float p = __builtin_amdgcn_exp2f(s[m][b][i] - mx[m]);
             add += p;
             s[m][b][i] = p;
           }
-        sum[m] = sum[m] * scale + add;
-#pragma unroll
-        for (int d = 0; d < NDB; ++d) o[m][d] *= scale;
+        sum[m] += add;
       }
 
       if (more) wait_copies<NC>();  // (the last tile has nothing newer under way)
@@ -700,10 +708,7 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
 // the 32x32x16 product.  A wave forms the scores of tile t + 1 while it takes
 // the softmax of tile t, so that its vector work runs under its matrix work;
 // K of tile t + 2 and V of tile t + 1 are on their way meanwhile, with one
-// barrier a tile.  The running maximum of a row is raised only when a score
-// exceeds it by 2^8 (kSlack): probabilities then stay below 2^8 and the
-// output's accumulators are rescaled in few tiles.
-constexpr float kSlack = 8.f;
+// barrier a tile.
 
 template <int ST, int DH>
 struct ManyCfg {
