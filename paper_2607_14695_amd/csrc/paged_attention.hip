@@ -33,15 +33,16 @@ RFX_DEV Span span_of(const PagedAttnArgs& a, int pos, int len) {
   Span s;
   const int64_t cap = (int64_t)a.q.max_pages << a.c.shift;
   s.hi = (int)min((int64_t)(a.causal ? min(pos, len - 1) + 1 : len), cap);
-  s.lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+  s.lo = a.window > 0 ? (int)max((int64_t)0, (int64_t)pos - a.window + 1) : 0;
   return s;
 }
 
 // One (row, query head) by one wave, key by key, which reads nothing but what
-// the row sees; each lane holds DH / 64 dims.
+// the row sees; each lane holds DH / 64 dims.  Four keys' loads are under way at
+// a time.
 template <typename T, int DH>
 RFX_DEV void scalar_row(const PagedAttnArgs& a, int64_t row, int head, int b, Span sp, float& m, float& l, float* o) {
-  constexpr int N = DH / 64;
+  constexpr int N = DH / 64, U = 4;
   const int lane = threadIdx.x & 63;
   const T* qp = reinterpret_cast<const T*>(a.x.p) + row * a.x.rs + head * a.x.hs + lane * N;
   float q[N];
@@ -53,22 +54,53 @@ RFX_DEV void scalar_row(const PagedAttnArgs& a, int64_t row, int head, int b, Sp
   m = kFloor;
   l = 0.f;
   const int64_t hoff = (int64_t)(head / a.group) << a.c.shift;
-  for (int j = sp.lo; j < sp.hi; ++j) {
+  for (int j = sp.lo; j < sp.hi; j += U) {
+    int r[U];
+    float k[U][N], v[U][N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) r[u] = j + u < sp.hi ? page_row(a.c, a.q, b, j + u) : -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int64_t at = (max(r[u], 0) + hoff) * DH + lane * N + i;
+        k[u][i] = to_f(reinterpret_cast<const T*>(a.c.k)[at]);
+        v[u][i] = to_f(reinterpret_cast<const T*>(a.c.v)[at]);
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (r[u] < 0) continue;
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) s += q[i] * k[u][i];
+      s = warp_sum(s) * a.scale2;
+      const float m2 = fmaxf(m, s);
+      const float c = exp2f(m - m2), p = exp2f(s - m2);
+      m = m2;
+      l = l * c + p;
+#pragma unroll
+      for (int i = 0; i < N; ++i) o[i] = o[i] * c + p * v[u][i];
+    }
+  }
+}
+
+// Whether one of the present keys [lo, hi) has an infinity or a NaN among its
+// values.
+template <typename T, int DH>
+RFX_DEV bool values_not_finite(const PagedAttnArgs& a, int head, int b, int lo, int hi) {
+  constexpr int N = DH / 64;
+  const int lane = threadIdx.x & 63;
+  const int64_t hoff = (int64_t)(head / a.group) << a.c.shift;
+  for (int j = lo; j < hi; ++j) {
     const int r = page_row(a.c, a.q, b, j);
     if (r < 0) continue;
-    const T* kp = reinterpret_cast<const T*>(a.c.k) + (r + hoff) * DH + lane * N;
     const T* vp = reinterpret_cast<const T*>(a.c.v) + (r + hoff) * DH + lane * N;
-    float s = 0.f;
+    bool odd = false;
 #pragma unroll
-    for (int i = 0; i < N; ++i) s += q[i] * to_f(kp[i]);
-    s = warp_sum(s) * a.scale2;
-    const float m2 = fmaxf(m, s);
-    const float c = exp2f(m - m2), p = exp2f(s - m2);
-    m = m2;
-    l = l * c + p;
-#pragma unroll
-    for (int i = 0; i < N; ++i) o[i] = o[i] * c + p * to_f(vp[i]);
+    for (int i = 0; i < N; ++i) odd |= !(fabsf(to_f(vp[i])) < INFINITY);
+    if (__ballot(odd)) return true;
   }
+  return false;
 }
 
 // out[row][head] = o / l; each lane holds DH / 64 dims.
@@ -98,8 +130,8 @@ template <int N> RFX_DEV void lds_dma16_run(const void* base, const uint32_t (&o
   } else {
     asm volatile("s_mov_b32 m0, %5\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %4\n\t"
                  "global_load_lds_dwordx4 %1, %4 offset:1024\n\tglobal_load_lds_dwordx4 %2, %4 offset:2048\n\t"
-                 "global_load_lds_dwordx4 %3, %4 offset:3072"
-                 :: "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base), "s"(m0) : "memory");
+                 "global_load_lds_dwordx4 %3, %4 offset:%6"
+                 :: "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base), "s"(m0), "n"(3 * 1024) : "memory");
   }
 }
 
@@ -246,23 +278,28 @@ RFX_DEV bool find_tile(const PagedAttnArgs& a, int tile, int bm, int lane, Tile&
 // A row's result of one split: stored, or kept for the merge.  `mixed`: the
 // tile's rows do not all see the same keys, so a NaN or an infinity among the
 // values of a key that this row does not see has met a probability of 0 in the
-// matrix product.  Such a row is done again key by key, which reads only what
-// the row sees.  (Values in 8 bits are finite codes; their scales never meet a
-// probability of 0.)
+// matrix product.  `halves`: probabilities were taken as two bf16, of which the
+// second, being 0 or of either sign, makes a NaN of an infinite value.  A row
+// with such a result is done again key by key, which reads only what the row
+// sees.  Where the sum is not finite a score that the row does see was not, and
+// all of the row is NaN.  (Values in 8 bits are finite codes; their scales never
+// meet a probability of 0.)
 template <typename T, int ST, int DH>
 RFX_DEV void finish_row(const PagedAttnArgs& a, const Tile& t, int64_t row, int head, int pos, int k_beg, int k_end,
-                        int split, bool mixed, float M, float L, float* y) {
+                        int split, bool mixed, bool halves, float M, float L, float* y) {
   constexpr int N = DH / 64;
   constexpr bool Q8 = ST == REFLEX_STORE_FP8 || ST == REFLEX_STORE_INT8;
   if constexpr (!Q8) {
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < N; ++i) odd |= !(fabsf(y[i]) < INFINITY);
-    if (mixed && __ballot(odd)) {
+    if (__ballot(odd) && L < INFINITY && (mixed || halves)) {
       Span sp = span_of(a, pos, t.len);
       sp.lo = max(sp.lo, k_beg);
       sp.hi = min(sp.hi, k_end);
-      scalar_row<T, DH>(a, row, head, t.b, sp, M, L, y);
+      if (halves || values_not_finite<T, DH>(a, head, t.b, k_beg, min(sp.lo, k_end)) ||
+          values_not_finite<T, DH>(a, head, t.b, max(sp.hi, k_beg), k_end))
+        scalar_row<T, DH>(a, row, head, t.b, sp, M, L, y);
     }
   }
   if (a.nsplit == 1) {
@@ -693,8 +730,8 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
     }
     const int r = t.r0 + q, tok = r / a.group, head = kvh * a.group + (r - tok * a.group);
     const int64_t row = t.first_row + tok;
-    finish_row<T, ST, DH>(a, t, row, head, t.first_pos + tok, k_beg, k_end, split, lo_min != lo_max || hi_min != hi_max, M, L,
-                          y);
+    finish_row<T, ST, DH>(a, t, row, head, t.first_pos + tok, k_beg, k_end, split, lo_min != lo_max || hi_min != hi_max,
+                          BF, M, L, y);
   }
 }
 
@@ -1160,7 +1197,7 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
 #pragma unroll
     for (int i = 0; i < N; ++i) y[i] = ex[q * OP + lane * N + i];
     finish_row<T, ST, DH>(a, t, t.first_row + tq, kvh * a.group + (rq - tq * a.group), t.first_pos + tq, k_beg, k_end,
-                          split, mixed, w.x, w.y, y);
+                          split, mixed, false, w.x, w.y, y);
   }
 }
 

@@ -379,6 +379,60 @@ def test_what_is_not_seen_does_not_matter(dtype, dh, new, length, window):
         assert bool(torch.isposinf(got[-1, :, 3]).all() and got[-1, :, 4].isnan().all() and got[-1, :, 5:].isfinite().all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [64, 256])
+@pytest.mark.parametrize("new,length", [(1, 900), (6, 40), (70, 600)])
+def test_what_is_seen_and_not_finite_matters(dtype, dh, new, length):
+    """An infinity and a NaN among the values of a key that every row sees stay in their dimensions; a key that is not
+    finite makes all of the rows that see it NaN."""
+    gen = torch.Generator().manual_seed(29)
+    cu, lens, table, n_pages = pool([new], [length], 16, gen)
+    cache, k, v = filled(n_pages, 1, 16, dh, dtype, gen)
+    q = draw(gen, (new, 4, dh), dtype)
+    clean = check_attention(q, cache, (k, v), cu, lens, table, True, 0, dtype)
+    at = ref.place(table[0], n_pages, 16, 5)
+    cache.v[at[0], 0, at[1], 3] = float("-inf")
+    cache.v[at[0], 0, at[1], 4] = float("nan")
+    got = f64(cache.attend(batch(cu, lens, table), q.to(DEV)))
+    assert np.isneginf(got[..., 3]).all() and np.isnan(got[..., 4]).all()
+    # the same sums, at most in another order: each side is within check_attention's tolerance of the formula
+    np.testing.assert_allclose(np.delete(got, [3, 4], -1), np.delete(clean, [3, 4], -1),
+                               atol=0.05 if dtype == "bf16" else 1e-4)
+    cache.k[at[0], 0, at[1], 9] = float("nan")
+    assert bool(cache.attend(batch(cu, lens, table), q.to(DEV)).isnan().all())
+
+
+@pytest.mark.parametrize("new", [7, 90])
+def test_widest_window(new):
+    """The largest window masks nothing, also for rows before a sequence's start."""
+    gen = torch.Generator().manual_seed(31)
+    cu, lens, table, n_pages = pool([new, 3], [4, 60], 8, gen)
+    cache, k, v = filled(n_pages, 1, 8, 64, "f32", gen)
+    q = draw(gen, (new + 3, 2, 64), "f32")
+    got = check_attention(q, cache, (k, v), cu, lens, table, False, 2 ** 31 - 1, "f32")
+    assert np.abs(got[0]).max() > 0
+
+
+def test_no_pages_and_no_sequences():
+    """A table without columns holds no tokens; a batch without sequences touches nothing."""
+    cache = PagedCache.zeros(2, 8, 1, 64, torch.float32, DEV)
+    cache.k.fill_(3.0)
+    x = torch.ones(5, 1, 64, device=DEV)
+    none = batch(torch.tensor([0, 5], dtype=torch.int32), torch.tensor([5], dtype=torch.int32),
+                 torch.empty(1, 0, dtype=torch.int32))
+    out = torch.full((5, 2, 64), 7.0, device=DEV)
+    cache.write(none, x, x)
+    k, v = cache.read(none, 5, torch.float32)
+    cache.attend(none, x.expand(5, 2, 64).contiguous(), out=out)
+    assert bool((cache.k == 3.0).all()) and not bool(k.any() or v.any() or out.any())
+    empty = batch(torch.zeros(1, dtype=torch.int32), torch.empty(0, dtype=torch.int32),
+                  torch.empty(0, 4, dtype=torch.int32))
+    out.fill_(7.0)
+    cache.write(empty, x, x)
+    cache.attend(empty, x.expand(5, 2, 64).contiguous(), out=out)
+    assert bool((cache.k == 3.0).all() and (out == 7.0).all())
+
+
 @pytest.mark.parametrize("dtype,store", [("bf16", "fp8"), ("bf16", "int8"), ("f32", "fp8")])
 @pytest.mark.parametrize("dh", [64, 128, 256])
 @pytest.mark.parametrize("new,length,window", [(1, 40, 0), (70, 400, 0), (200, 700, 64)])
