@@ -329,6 +329,13 @@ RFX_DEV void finish_row(const PagedAttnArgs& a, const Tile& t, int64_t row, int 
 // 8-bit codes become bf16 exactly on the way from LDS; the keys' scales enter
 // the scores and the values' scales the probabilities, in fp32, so a code is
 // never rounded.  The waves' results meet in LDS at the end.
+//
+// 64 single tokens, 8 query heads of 256 on one K/V head: over 15,409 fp8 keys
+// at most (310 MB) 66-73 us, 4.2-4.7 TB/s; over 8,000 bf16 keys (525 MB) 104 us,
+// 5.0 TB/s, as a large copy.  One token over 817 keys 10 us, a chain of
+// latencies (lengths, table, K, V, the exchange).  fp32 is bound by its matrix
+// products at one wave to a SIMD: four prompts of 1,000 rows with 8 heads of 128
+// 356 us, 69 TFLOP/s of the 154 that a large fp32 product reaches.
 template <typename T, int ST, int DH>
 struct FewCfg {
   static constexpr bool Q8 = ST == REFLEX_STORE_FP8 || ST == REFLEX_STORE_INT8;
@@ -745,8 +752,16 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
 // the 32x32x16 product.  A wave forms the scores of tile t + 1 while it takes
 // the softmax of tile t, so that its vector work runs under its matrix work;
 // K of tile t + 2 and V of tile t + 1 are on their way meanwhile, with one
-// barrier a tile.
-
+// barrier a tile.  The probabilities are rounded to bf16 once (two halves, as
+// with few rows, would double the second product).
+//
+// Two prompts of 8,192 rows with 32 heads of 128, causal: 1.13-1.17 ms, 940-970
+// TFLOP/s, matrix units busy for 53 % and vector issue for 56 % of the cycles
+// (the exponentials, maxima and roundings that cannot all hide).  One chunk of
+// 768 rows with 8 heads of 256 over 15,408 keys: 122 us, 790 TFLOP/s; the
+// products alone, by the single wave that a SIMD holds, take 96.  8-bit pages
+// cost a conversion of every fragment in every wave: prompts 1.37 (fp8) and
+// 1.71 ms (int8).
 template <int ST, int DH>
 struct ManyCfg {
   static constexpr bool Q8 = ST == REFLEX_STORE_FP8 || ST == REFLEX_STORE_INT8;
@@ -1203,7 +1218,7 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
 
 // One wave per (row, head): the splits' partial results joined in order.  Those
 // of the first eight splits are requested with the maxima and sums, so that
-// most rows take one memory round trip: 6,144 rows of 256 in five splits 7 us,
+// most rows take one memory round trip: 6,144 rows of 256 in five splits 8 us,
 // 32 MB of partial results.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void paged_attn_merge_kernel(const PagedAttnArgs a) {
@@ -1260,17 +1275,20 @@ int64_t tile_bound(int64_t n_rows, int n_seqs, int group, int bm) {
 // 32 with the few-row kernel, 128 with the many-row one.  fp32, which only the
 // first has, takes 32 where that makes two workgroups for every CU: seven
 // ragged chunks of up to 450 rows 28 us with 16 against 40, four of 4,000 rows
-// 461 against 392.
-int rows_of_tile(int64_t n_rows, int n_seqs, int group, int n_kv, int dtype) {
+// 430 against 360.  256-wide heads stay at 16, as queries and sums of 32 such
+// rows do not fit a wave's registers: four of 8,000 rows 755 us against 882,
+// over int8 pages 600 against 742.
+int rows_of_tile(int64_t n_rows, int n_seqs, int group, int n_kv, int dh, int dtype) {
   const int64_t rows = n_rows * group / std::max<int64_t>(1, std::min<int64_t>(n_seqs, n_rows));
   if (rows <= 16) return 16;
-  if (dtype != REFLEX_DTYPE_BF16) return tile_bound(n_rows, n_seqs, group, 32) * n_kv >= 512 ? 32 : 16;
+  if (dtype != REFLEX_DTYPE_BF16) return dh <= 128 && tile_bound(n_rows, n_seqs, group, 32) * n_kv >= 512 ? 32 : 16;
   return rows <= 32 ? 32 : 128;
 }
 
 template <typename T, int ST, int DH>
 hipError_t launch_shape(const PagedAttnArgs& a, hipStream_t s) {
-  const int bm = rows_of_tile(a.n_rows, a.q.n, a.group, a.c.n_kv, sizeof(T) == 2 ? REFLEX_DTYPE_BF16 : REFLEX_DTYPE_F32);
+  const int bm = rows_of_tile(a.n_rows, a.q.n, a.group, a.c.n_kv, DH,
+                              sizeof(T) == 2 ? REFLEX_DTYPE_BF16 : REFLEX_DTYPE_F32);
   const int64_t tiles = tile_bound(a.n_rows, a.q.n, a.group, bm);
   const dim3 grid((unsigned)tiles, (unsigned)(a.c.n_kv * a.nsplit));
   if constexpr (sizeof(T) == 2) {
@@ -1281,8 +1299,9 @@ hipError_t launch_shape(const PagedAttnArgs& a, hipStream_t s) {
   }
   if (bm == 16)
     RFX_LAUNCH((paged_attn_few_kernel<T, ST, DH, 1>), grid, dim3(256), 0, s, a);
-  else if (bm == 32)
-    RFX_LAUNCH((paged_attn_few_kernel<T, ST, DH, 2>), grid, dim3(256), 0, s, a);
+  if constexpr (sizeof(T) == 2 || DH <= 128) {
+    if (bm == 32) RFX_LAUNCH((paged_attn_few_kernel<T, ST, DH, 2>), grid, dim3(256), 0, s, a);
+  }
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.nsplit > 1) {
     RFX_LAUNCH((paged_attn_merge_kernel<T, DH>), dim3((unsigned)((a.n_rows * a.n_q + 3) / 4)), dim3(256), 0, s, a);
@@ -1306,11 +1325,11 @@ PagedAttnPlan paged_attention_plan(const reflex_paged_cache& c, const reflex_pag
   const int group = n_q / c.n_kv_heads;
   const int64_t cap = (int64_t)b.max_pages * c.page_size;
   const int64_t len = b.max_length > 0 && b.max_length < cap ? b.max_length : cap;
-  const int bm = rows_of_tile(n_rows, b.n_seqs, group, c.n_kv_heads, dtype);
+  const int bm = rows_of_tile(n_rows, b.n_seqs, group, c.n_kv_heads, c.head_dim, dtype);
   // Workgroups without a split, were the sequences alike.  Splits make one round
   // of two workgroups to a CU of them (the widest many-row kernel: of one), each
-  // with 128 keys at least: 64 single tokens over 15,409 fp8 keys 78 us with 8
-  // splits against 88 with 11 and 87 with 6.
+  // with 128 keys at least: 64 single tokens over 15,409 fp8 keys took 78 us with
+  // 8 splits against 88 with 11 and 87 with 6.
   const int64_t seqs = std::max<int64_t>(1, std::min<int64_t>(b.n_seqs, n_rows));
   const int64_t blocks = seqs * ((n_rows * group + seqs * bm - 1) / (seqs * bm)) * c.n_kv_heads;
   const int64_t slots = bm == 128 && c.head_dim > 128 ? 256 : 512;

@@ -75,6 +75,9 @@ RFX_DEV void turns_of(const reflex_rotary& plan, const int64_t* pos, int64_t ps,
 // ---------------------------------------------------------------------------
 // rotary
 // ---------------------------------------------------------------------------
+// 24,576 rows of 8 heads of 256 in fp32 (403 MB read and written) take 86 us,
+// 4.7 TB/s, where a large copy reaches 4.9; 768 rows in bf16 5 us and eight rows
+// 4 us, the latency of positions, frequencies and rows.
 template <typename T>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
   const int G = a.plan.head_dim >> 4;
@@ -251,7 +254,9 @@ template <> struct Raw8<bf16_t> {
 
 // blockIdx.z: 0 = K (rotated), 1 = V.  A wave takes 64 / G rows.  Bound by the
 // vector unit where keys are rotated for an 8-bit store: 32 frames of 768 keys
-// of 256 take 21 us with V, 8 us of them memory's.  (Measured slower: four times
+// of 256 take 20 us with V, 8 us of them memory's.  Eight prompts with eight
+// heads of 128 (44,000 rows, 273 MB) 70 us, 3.9 TB/s: the angles' sines are taken
+// once for all heads.  (Measured slower: four times
 // the rows a wave, 22 us and, with eight 128-wide heads, 89 against 78 us; K and
 // V side by side in turn, 25 us.)
 template <typename T, int ST>
@@ -373,7 +378,8 @@ RFX_DEV void decode8(const uint2& c, float scale, float* o) {
 }
 
 // blockIdx.z: 0 = K, 1 = V; blockIdx.y: the head.  A wave takes U times 64 / G
-// rows, whose loads are all under way before the first is used.
+// rows, whose loads are all under way before the first is used.  The same prompts
+// 50 us, 5.4 TB/s.
 template <typename T, int ST, int U>
 __global__ __launch_bounds__(256) void paged_read_kernel(const PagedReadArgs a) {
   constexpr bool Q = ST == REFLEX_STORE_FP8 || ST == REFLEX_STORE_INT8;

@@ -312,6 +312,18 @@ def test_attention(case, dtype, store):
     check_attention(q, cache, (k, v), cu, lens, table, causal, window, dtype)
 
 
+@pytest.mark.parametrize("store", ["f32", "fp8", "int8"])
+@pytest.mark.parametrize("dh,window", [(64, 0), (128, 21), (256, 0)])
+def test_fp32_tiles_of_many_chunks(store, dh, window):
+    """Enough short chunks for the wider fp32 tiles, two of them to a chunk in one sequence."""
+    gen = torch.Generator().manual_seed(dh + window)
+    seqs = [(9, 9 + 7 * i % 70) for i in range(270)] + [(20, 75), (0, 4), (1, 1)]
+    cu, lens, table, n_pages = pool([s[0] for s in seqs], [s[1] for s in seqs], 8, gen)
+    cache, k, v = filled(n_pages, 2, 8, dh, store, gen)
+    q = draw(gen, (int(cu[-1]), 4, dh), "f32")
+    check_attention(q, cache, (k, v), cu, lens, table, True, window, "f32")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("dh", [64, 128, 256])
 def test_attention_strided_rows_and_rows_of_no_sequence(dtype, dh):
