@@ -100,16 +100,15 @@ struct PagedAttnArgs {
   int negate;        // scale < 0: queries enter with the other sign
   int causal, window;
   int nsplit;        // key splits; with more than one, partials go to the workspace
-  int split_keys;    // keys per split (the last one takes all that is left)
   float* part_o;     // [n_rows * n_q][nsplit][dh]
   float2* part_ml;   // [n_rows * n_q][nsplit] (running maximum, sum)
 };
 struct PagedAttnPlan {
-  int nsplit, split_keys;
+  int nsplit;
   size_t bytes;
 };
 PagedAttnPlan paged_attention_plan(const reflex_paged_cache& c, const reflex_paged_batch& b, int64_t n_rows, int n_q,
-                                   int dtype);
+                                   int dtype, int window);
 template <typename T> hipError_t launch_paged_attention(const PagedAttnArgs& a, int store, hipStream_t s);
 
 }  // namespace reflex

@@ -207,7 +207,7 @@ int reflex_paged_attention_workspace(const reflex_paged_cache* cache, const refl
   RFX_CHECK(check_store(cache, dtype));
   if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads || n_rows * (int64_t)n_q_heads > (int64_t(1) << 23))
     return REFLEX_EINVAL;
-  *bytes = n_rows == 0 || batch->n_seqs == 0 ? 0 : paged_attention_plan(*cache, *batch, n_rows, n_q_heads, dtype).bytes;
+  *bytes = n_rows == 0 || batch->n_seqs == 0 ? 0 : paged_attention_plan(*cache, *batch, n_rows, n_q_heads, dtype, 0).bytes;
   return REFLEX_OK;
 }
 
@@ -221,7 +221,7 @@ int reflex_paged_attention(const reflex_paged_cache* cache, const reflex_paged_b
   if (!isfinite(scale) || window < 0) return REFLEX_EINVAL;
   if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return REFLEX_EINVAL;
   if (n_rows == 0 || batch->n_seqs == 0) return REFLEX_OK;
-  const PagedAttnPlan p = paged_attention_plan(*cache, *batch, n_rows, n_q_heads, dtype);
+  const PagedAttnPlan p = paged_attention_plan(*cache, *batch, n_rows, n_q_heads, dtype, window);
   PagedAttnArgs a;
   a.c = pages_of(cache);
   a.q = seqs_of(batch);
@@ -235,7 +235,6 @@ int reflex_paged_attention(const reflex_paged_cache* cache, const reflex_paged_b
   a.causal = causal != 0;
   a.window = window;
   a.nsplit = p.nsplit;
-  a.split_keys = p.split_keys;
   const size_t rows = (size_t)n_rows * n_q_heads * p.nsplit;
   a.part_o = reinterpret_cast<float*>(workspace);
   a.part_ml = reinterpret_cast<float2*>(reinterpret_cast<char*>(workspace) + rows * cache->head_dim * sizeof(float));
