@@ -289,6 +289,18 @@ RFX_DEV bool find_tile(const PagedAttnArgs& a, int tile, int bm, int lane, Tile&
 }
 
 
+// How many such tiles the batch has: at most tile_bound.
+RFX_DEV int count_tiles(const PagedAttnArgs& a, int bm, int lane) {
+  int sum = 0;
+  for (int b = lane; b < a.q.n; b += 64) {
+    const int c0 = (int)min((int64_t)max(a.q.cu[b], 0), a.n_rows), c1 = (int)min((int64_t)max(a.q.cu[b + 1], 0), a.n_rows);
+    sum += c1 > c0 ? ((c1 - c0) * a.group + bm - 1) / bm : 0;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  return __builtin_amdgcn_readfirstlane(sum);
+}
+
 // A row's result of one split: stored, or kept for the merge.  `mixed`: the
 // tile's rows do not all see the same keys, so a NaN or an infinity among the
 // values of a key that this row does not see has met a probability of 0 in the
@@ -790,7 +802,7 @@ struct ManyCfg {
 };
 
 template <int ST, int DH>
-__global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel(const PagedAttnArgs a, int tiles) {
+__global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel(const PagedAttnArgs a, int grid_tiles) {
   typedef ManyCfg<ST, DH> C;
   typedef bf16_t T;
   constexpr bool Q8 = C::Q8;
@@ -812,11 +824,16 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
   const int r32 = lane & 31, h = lane >> 5;
   // consecutive workgroups go to the eight XCDs in turn: each XCD takes a run
   // of (head, split) groups, so that a group's tiles share its L2, and a
-  // group's last tiles (with a causal mask the longest) first
-  const int per = gridDim.x >> 3;
+  // group's last tiles (with a causal mask the longest) first.  One workgroup to
+  // a CU may fill the chip exactly, and then the runs have to be of the tiles
+  // that the batch has, not of the grid's: with those a chunk of 1,024 rows of 8
+  // heads over 8,192 keys gave some XCDs one too many and took 159 us instead of
+  // 93.  (Narrower heads, two workgroups to a CU, lose 2 % to the counting.)
+  const int tiles = WIDE ? count_tiles(a, BM, lane) : grid_tiles;
+  const int all = tiles * a.c.n_kv * a.nsplit, per = (all + 7) >> 3;
   const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per || id >= all) return;
   const int grp = id / tiles;
-  if (grp >= a.c.n_kv * a.nsplit) return;
   const int kvh = grp / a.nsplit, split = grp - kvh * a.nsplit;
   Tile t;
   if (!find_tile(a, tiles - 1 - (id - grp * tiles), BM, lane, t)) return;
