@@ -1302,7 +1302,7 @@ int64_t tile_bound(int64_t n_rows, int n_seqs, int group, int bm) {
 // Rows of a tile, by the rows of an average sequence (with one K/V head): 16 or
 // 32 with the few-row kernel, 128 with the many-row one.  fp32, which only the
 // first has, takes 32 where that makes two workgroups for every CU: seven
-// ragged chunks of up to 450 rows 28 us with 16 against 40, four of 4,000 rows
+// ragged chunks of up to 450 rows 23 us with 16 against 30, four of 4,000 rows
 // 430 against 360.  256-wide heads stay at 16, as queries and sums of 32 such
 // rows do not fit a wave's registers: four of 8,000 rows 755 us against 882,
 // over int8 pages 600 against 742.
