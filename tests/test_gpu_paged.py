@@ -312,6 +312,28 @@ def test_attention(case, dtype, store):
     check_attention(q, cache, (k, v), cu, lens, table, causal, window, dtype)
 
 
+@pytest.mark.parametrize("dtype,store", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32")])
+@pytest.mark.parametrize("window,max_length", [(600, 0), (129, 300), (2900, 0)])
+def test_splits_of_a_window(dtype, store, window, max_length):
+    """Single tokens whose windows are split, at any place of the sequence and beyond the expected length."""
+    gen = torch.Generator().manual_seed(window)
+    cu, lens, table, n_pages = pool([1, 1, 2, 1, 1], [5000, 3, 700, 1281, 0], 16, gen)
+    cache, k, v = filled(n_pages, 2, 16, 128, store, gen)
+    q = draw(gen, (6, 4, 128), dtype)
+    check_attention(q, cache, (k, v), cu, lens, table, True, window, dtype, max_length=max_length)
+
+
+@pytest.mark.parametrize("store", ["bf16", "int8"])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 150)])
+def test_wide_heads_of_ragged_chunks(store, causal, window):
+    """256-wide heads with many rows, fewer tiles than the launch has room for, some in splits."""
+    gen = torch.Generator().manual_seed(37)
+    cu, lens, table, n_pages = pool([0, 70, 0, 200, 1, 129, 0], [5, 210, 9, 900, 300, 129, 40], 16, gen)
+    cache, k, v = filled(n_pages, 2, 16, 256, store, gen)
+    q = draw(gen, (int(cu[-1]), 4, 256), "bf16")
+    check_attention(q, cache, (k, v), cu, lens, table, causal, window, "bf16")
+
+
 @pytest.mark.parametrize("store", ["f32", "fp8", "int8"])
 @pytest.mark.parametrize("dh,window", [(64, 0), (128, 21), (256, 0)])
 def test_fp32_tiles_of_many_chunks(store, dh, window):
