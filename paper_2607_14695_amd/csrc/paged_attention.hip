@@ -51,10 +51,20 @@ RFX_DEV Span split_of(const PagedAttnArgs& a, int lo, int hi, int split) {
   return s;
 }
 
+template <int ST> RFX_DEV float code_to_f32(uint32_t c) {
+  return ST == REFLEX_STORE_FP8 ? __builtin_amdgcn_cvt_f32_fp8((int)c, 0) : (float)(int8_t)c;
+}
+
+// Element `at` of the pages as fp32, without its row's scale.
+template <typename T, int ST> RFX_DEV float page_elem(const char* p, int64_t at) {
+  if constexpr (ST == REFLEX_STORE_FP8) return code_to_f32<ST>(reinterpret_cast<const uint8_t*>(p)[at]);
+  else return to_f(reinterpret_cast<const T*>(p)[at]);
+}
+
 // One (row, query head) by one wave, key by key, which reads nothing but what
 // the row sees; each lane holds DH / 64 dims.  Four keys' loads are under way at
 // a time.
-template <typename T, int DH>
+template <typename T, int ST, int DH>
 RFX_DEV void scalar_row(const PagedAttnArgs& a, int64_t row, int head, int b, Span sp, float& m, float& l, float* o) {
   constexpr int N = DH / 64, U = 4;
   const int lane = threadIdx.x & 63;
@@ -70,37 +80,40 @@ RFX_DEV void scalar_row(const PagedAttnArgs& a, int64_t row, int head, int b, Sp
   const int64_t hoff = (int64_t)(head / a.group) << a.c.shift;
   for (int j = sp.lo; j < sp.hi; j += U) {
     int r[U];
-    float k[U][N], v[U][N];
+    float k[U][N], v[U][N], ks[U], vs[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) r[u] = j + u < sp.hi ? page_row(a.c, a.q, b, j + u) : -1;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      const int64_t pr = max(r[u], 0) + hoff;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int64_t at = (max(r[u], 0) + hoff) * DH + lane * N + i;
-        k[u][i] = to_f(reinterpret_cast<const T*>(a.c.k)[at]);
-        v[u][i] = to_f(reinterpret_cast<const T*>(a.c.v)[at]);
+        k[u][i] = page_elem<T, ST>(a.c.k, pr * DH + lane * N + i);
+        v[u][i] = page_elem<T, ST>(a.c.v, pr * DH + lane * N + i);
       }
+      ks[u] = ST == REFLEX_STORE_FP8 ? a.c.k_scale[pr] : 1.f;
+      vs[u] = ST == REFLEX_STORE_FP8 ? a.c.v_scale[pr] : 1.f;
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (r[u] < 0) continue;
       float s = 0.f;
 #pragma unroll
       for (int i = 0; i < N; ++i) s += q[i] * k[u][i];
-      s = warp_sum(s) * a.scale2;
+      s = warp_sum(s) * a.scale2 * ks[u];
       const float m2 = fmaxf(m, s);
       const float c = exp2f(m - m2), p = exp2f(s - m2);
       m = m2;
       l = l * c + p;
 #pragma unroll
-      for (int i = 0; i < N; ++i) o[i] = o[i] * c + p * v[u][i];
+      for (int i = 0; i < N; ++i) o[i] = o[i] * c + p * vs[u] * v[u][i];
     }
   }
 }
 
 // Whether one of the present keys [lo, hi) has an infinity or a NaN among its
-// values.
-template <typename T, int DH>
+// values (in fp8 a NaN among its codes).
+template <typename T, int ST, int DH>
 RFX_DEV bool values_not_finite(const PagedAttnArgs& a, int head, int b, int lo, int hi) {
   constexpr int N = DH / 64;
   const int lane = threadIdx.x & 63;
@@ -108,10 +121,10 @@ RFX_DEV bool values_not_finite(const PagedAttnArgs& a, int head, int b, int lo, 
   for (int j = lo; j < hi; ++j) {
     const int r = page_row(a.c, a.q, b, j);
     if (r < 0) continue;
-    const T* vp = reinterpret_cast<const T*>(a.c.v) + (r + hoff) * DH + lane * N;
     bool odd = false;
 #pragma unroll
-    for (int i = 0; i < N; ++i) odd |= !(fabsf(to_f(vp[i])) < INFINITY);
+    for (int i = 0; i < N; ++i)
+      odd |= !(fabsf(page_elem<T, ST>(a.c.v, (r + hoff) * DH + lane * N + i)) < INFINITY);
     if (__ballot(odd)) return true;
   }
   return false;
@@ -235,9 +248,6 @@ template <int ST> RFX_DEV uint4 codes_to_bf16(uint2 c) {
 }
 
 // codes -> fp32
-template <int ST> RFX_DEV float code_to_f32(uint32_t c) {
-  return ST == REFLEX_STORE_FP8 ? __builtin_amdgcn_cvt_f32_fp8((int)c, 0) : (float)(int8_t)c;
-}
 template <int ST> RFX_DEV uint4 codes_to_f32(uint32_t c) {
   float f[4];
 #pragma unroll
@@ -301,32 +311,50 @@ RFX_DEV int count_tiles(const PagedAttnArgs& a, int bm, int lane) {
   return __builtin_amdgcn_readfirstlane(sum);
 }
 
-// A row's result of one split: stored, or kept for the merge.  `mixed`: the
-// tile's rows do not all see the same keys, so a NaN or an infinity among the
-// values of a key that this row does not see has met a probability of 0 in the
-// matrix product.  `halves`: probabilities were taken as two bf16, of which the
-// second, being 0 or of either sign, makes a NaN of an infinite value.  A row
-// with such a result is done again key by key, which reads only what the row
-// sees.  Where the sum is not finite a score that the row does see was not, and
-// all of the row is NaN.  (Values in 8 bits are finite codes; their scales never
-// meet a probability of 0.)
+// Row `q` of a tile done again where its result is not finite: key by key, which
+// reads only what the row sees.  Needed where a key that this row does not see,
+// but another row of the tile does, has a value that is not finite, which has met
+// a probability of 0 in the matrix product; and with `halves`, probabilities
+// taken as two bf16, of which the second, being 0 or of either sign, makes a NaN
+// of an infinite value.  (Codes in fp8 are finite or NaN, in int8 finite; the
+// scale of a value that the row does not see never meets its probability of 0.)
+//
+// All of it starts from the arguments (the kernel's first parameter lies at the
+// start of the argument segment) and the tile's number, so that this rare path
+// keeps nothing alive through the loops before it: what it needs held from there
+// cost 29 spilled scalar registers and 5 to 8 % with many rows over fp8 pages.
 template <typename T, int ST, int DH>
-RFX_DEV void finish_row(const PagedAttnArgs& a, const Tile& t, int64_t row, int head, int pos, int k_beg, int k_end,
-                        int split, bool mixed, bool halves, float M, float L, float* y) {
+RFX_DEV void redo_row(int tile, int bm, int q, int64_t row, int head, int split, bool halves, float& M, float& L,
+                      float* y) {
+  uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  const PagedAttnArgs& a = *reinterpret_cast<const PagedAttnArgs*>(at);
+  Tile t;
+  if (!find_tile(a, tile, bm, threadIdx.x & 63, t)) return;
+  const int last = min(bm, t.rows - t.r0) - 1;
+  const Span first_sees = span_of(a, t.first_pos + t.r0 / a.group, t.len);
+  const Span last_sees = span_of(a, t.first_pos + (t.r0 + last) / a.group, t.len);
+  const Span part = split_of(a, first_sees.lo, last_sees.hi, split);
+  Span sp = span_of(a, t.first_pos + (t.r0 + q) / a.group, t.len);
+  sp.lo = max(sp.lo, part.lo);
+  sp.hi = min(sp.hi, part.hi);
+  if ((halves && ST != REFLEX_STORE_FP8) ||
+      values_not_finite<T, ST, DH>(a, head, t.b, part.lo, min(sp.lo, part.hi)) ||
+      values_not_finite<T, ST, DH>(a, head, t.b, max(sp.hi, part.lo), part.hi))
+    scalar_row<T, ST, DH>(a, row, head, t.b, sp, M, L, y);
+}
+
+// A row's result of one split: stored, or kept for the merge.  Where the sum is
+// not finite a score that the row does see was not, and all of the row is NaN.
+template <typename T, int ST, int DH>
+RFX_DEV void finish_row(const PagedAttnArgs& a, int tile, int bm, int q, int64_t row, int head, int split, bool halves,
+                        float M, float L, float* y) {
   constexpr int N = DH / 64;
-  constexpr bool Q8 = ST == REFLEX_STORE_FP8 || ST == REFLEX_STORE_INT8;
-  if constexpr (!Q8) {
+  if constexpr (ST != REFLEX_STORE_INT8) {
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < N; ++i) odd |= !(fabsf(y[i]) < INFINITY);
-    if (__ballot(odd) && L < INFINITY && (mixed || halves)) {
-      Span sp = span_of(a, pos, t.len);
-      sp.lo = max(sp.lo, k_beg);
-      sp.hi = min(sp.hi, k_end);
-      if (halves || values_not_finite<T, DH>(a, head, t.b, k_beg, min(sp.lo, k_end)) ||
-          values_not_finite<T, DH>(a, head, t.b, max(sp.hi, k_beg), k_end))
-        scalar_row<T, DH>(a, row, head, t.b, sp, M, L, y);
-    }
+    if (__ballot(odd) && L < INFINITY) redo_row<T, ST, DH>(tile, bm, q, row, head, split, halves, M, L, y);
   }
   if (a.nsplit == 1) {
     store_row<T, DH>(a, row, head, L, y);
@@ -761,8 +789,7 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
     }
     const int r = t.r0 + q, tok = r / a.group, head = kvh * a.group + (r - tok * a.group);
     const int64_t row = t.first_row + tok;
-    finish_row<T, ST, DH>(a, t, row, head, t.first_pos + tok, k_beg, k_end, split, lo_min != lo_max || hi_min != hi_max,
-                          BF, M, L, y);
+    finish_row<T, ST, DH>(a, blockIdx.x, BM, q, row, head, split, BF, M, L, y);
   }
 }
 
@@ -836,7 +863,8 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
   const int grp = id / tiles;
   const int kvh = grp / a.nsplit, split = grp - kvh * a.nsplit;
   Tile t;
-  if (!find_tile(a, tiles - 1 - (id - grp * tiles), BM, lane, t)) return;
+  const int tile = tiles - 1 - (id - grp * tiles);
+  if (!find_tile(a, tile, BM, lane, t)) return;
 
   const int rows_here = min(BM, t.rows - t.r0);
   const int p0 = t.first_pos + t.r0 / a.group, p1 = t.first_pos + (t.r0 + rows_here - 1) / a.group;
@@ -1232,15 +1260,14 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
           make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
   __syncthreads();
   constexpr int N = DH / 64;
-  const bool mixed = sp0.lo != sp1.lo || sp0.hi != sp1.hi;
   for (int q = 0; q < 32 && 32 * wave + q < rows_here; ++q) {
     const int rq = t.r0 + 32 * wave + q, tq = rq / a.group;
     const float2 w = ml[32 * wave + q];
     float y[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) y[i] = ex[q * OP + lane * N + i];
-    finish_row<T, ST, DH>(a, t, t.first_row + tq, kvh * a.group + (rq - tq * a.group), t.first_pos + tq, k_beg, k_end,
-                          split, mixed, false, w.x, w.y, y);
+    finish_row<T, ST, DH>(a, tile, BM, 32 * wave + q, t.first_row + tq, kvh * a.group + (rq - tq * a.group), split, false,
+                          w.x, w.y, y);
   }
 }
 

@@ -715,3 +715,54 @@ def test_python_refusals_on_the_gpu():
         cache.write(b, ok, ok, rotary=Rotary(64), positions=torch.zeros(3, dtype=torch.int64, device=DEV))
     with pytest.raises(ValueError):
         cache.write(b, ok, ok, rotary=Rotary(64), positions=torch.zeros(2, dtype=torch.int32, device=DEV))
+
+
+# ---------------------------------------------------------------------------
+# codes and scales that are not numbers
+# ---------------------------------------------------------------------------
+def attend_ref(q, k, v, cu, lens, table, window, dtype, scale=None, prob=None):
+    """(result, tolerance) of causal attention: the bound of check_attention; `prob`: what a probability's own
+    rounding may be off by, where it is less than a step of dtype."""
+    scale = q.shape[-1] ** -0.5 if scale is None else scale
+    want, spread, reach = ref.attend(f64(q), k, v, cu.numpy(), lens.numpy(), table.numpy(), True, window, scale)
+    prob = (2.0 ** -8 if dtype == "bf16" else 0) if prob is None else prob
+    moved = 2 * (2 * (q.shape[-1] + 4) * 2.0 ** -24 * reach + 2.0 ** -21 + 64 * 2.0 ** -24) + prob
+    under = 2.0 ** -126 * (1 + max(int(lens.max()), 0) * np.abs(v).max())
+    return want, moved * spread + ROUND[dtype] * np.abs(want) + under
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [64, 128, 256])
+@pytest.mark.parametrize("new,length,window", [(1, 40, 0), (6, 40, 0), (70, 170, 0), (200, 700, 64), (16, 4000, 1000)])
+def test_nan_codes_keep_to_the_rows_that_see_them(dtype, dh, new, length, window):
+    """e4m3 codes that are NaN: in every slot that no row sees, and in V or K of a token that the last rows see, or
+    the first ones."""
+    gen = torch.Generator().manual_seed(dh + new)
+    cu, lens, table, n_pages = pool([new], [length], 16, gen)
+    cache, k, v = filled(n_pages, 1, 16, dh, "fp8", gen)
+    first = max(0, length - new - window + 1) if window else 0
+    hide = torch.ones(n_pages, 16, dtype=torch.bool)
+    for j in range(first, length):
+        hide[ref.place(table[0], n_pages, 16, j)] = False
+    for t in (cache.k, cache.v):
+        t.view(torch.uint8)[:, 0][hide.to(DEV)] = 0x7F
+    q = draw(gen, (new, 2, dh), dtype)
+    b, pos = batch(cu, lens, table), np.arange(length - new, length)
+    want, tol = attend_ref(q, k, v, cu, lens, table, window, dtype)
+    assert np.all(np.abs(f64(cache.attend(b, q.to(DEV), window=window)) - want) <= tol)
+    for key in (max(length - 3, length - new), first):
+        see = (pos >= key) & ((pos < key + window) if window else True)
+        page, slot = ref.place(table[0], n_pages, 16, key)
+        kept = [t.view(torch.uint8)[page, 0, slot].clone() for t in (cache.k, cache.v)]
+        codes = cache.v.view(torch.uint8)[page, 0, slot]
+        codes[3], codes[dh - 2] = 0x7F, 0xFF
+        got = f64(cache.attend(b, q.to(DEV), window=window))
+        bad = np.zeros(got.shape, dtype=bool)
+        bad[see, :, 3] = bad[see, :, dh - 2] = True
+        np.testing.assert_array_equal(np.isnan(got), bad)
+        assert np.all((np.abs(got - want) <= tol)[~bad])
+        cache.k.view(torch.uint8)[page, 0, slot, 7] = 0xFF
+        got = f64(cache.attend(b, q.to(DEV), window=window))
+        assert np.isnan(got[see]).all() and np.all((np.abs(got - want) <= tol)[~see])
+        for t, old in zip((cache.k, cache.v), kept):
+            t.view(torch.uint8)[page, 0, slot] = old
