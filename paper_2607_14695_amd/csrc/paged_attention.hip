@@ -623,10 +623,14 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
 
       // softmax: scores in units of log2 e
       const bool whole = key0 >= max(lo_max, k_beg) && key0 + KT <= min(hi_min, k_end) && present == kAll;
+      // whether row m sees key `at` of the tile
+      auto sees = [&](int m, int at) __attribute__((always_inline)) {
+        const int key = key0 + at;
+        return key >= max(lo[m], k_beg) && key < min(hi[m], seg_end) && ((present >> at) & 1);
+      };
 #pragma unroll
       for (int m = 0; m < MR; ++m) {
         float top = kFloor;
-        const int l0 = max(lo[m], k_beg), h0 = min(hi[m], seg_end);
 #pragma unroll
         for (int b = 0; b < NKB; ++b) {
           const float kk[4] = {ks[b].x, ks[b].y, ks[b].z, ks[b].w};
@@ -634,11 +638,7 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
           for (int i = 0; i < 4; ++i) {
             float v = s[m][b][i] * scale2;
             if (Q8) v *= kk[i];
-            if (!whole) {
-              const int at = 16 * b + 4 * g + i, key = key0 + at;
-              const bool see = key >= l0 && key < h0 && ((present >> at) & 1);
-              v = see ? v : -INFINITY;
-            }
+            if (!whole) v = sees(m, 16 * b + 4 * g + i) ? v : -INFINITY;
             s[m][b][i] = v;
             top = fmaxf(top, v);
           }
@@ -674,12 +674,16 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
 #pragma unroll
           for (int m = 0; m < MR; ++m)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float p = s[m][b][i];
-              // (a key that the row does not see may have any scale)
-              s[m][b][i] = whole || p > 0.f || p != p ? p * vv[i] : 0.f;
-            }
+            for (int i = 0; i < 4; ++i) s[m][b][i] *= vv[i];
         }
+      }
+      if (Q8 && !whole) {  // a key that the row does not see may have any scale
+#pragma unroll
+        for (int m = 0; m < MR; ++m)
+#pragma unroll
+          for (int b = 0; b < NKB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[m][b][i] = sees(m, 16 * b + 4 * g + i) ? s[m][b][i] : 0.f;
       }
       // O^T += V^T P^T
       if (BF) {
@@ -1078,7 +1082,7 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
     };
     // probabilities of registers 2 (q % 8) and the next of block q / 8; the
     // empty statement keeps them at their place among the products
-    auto pair = [&](int x, bool whole, int q, const f32x16_v (&s)[2], uint32_t (&pw)[16]) __attribute__((always_inline)) {
+    auto pair = [&](int x, int q, const f32x16_v (&s)[2], uint32_t (&pw)[16]) __attribute__((always_inline)) {
       const int i = 2 * (q & 7);
       float p0 = __builtin_amdgcn_exp2f(fmaf(s[q >> 3][i], scale2, -mx));
       float p1 = __builtin_amdgcn_exp2f(fmaf(s[q >> 3][i + 1], scale2, -mx));
@@ -1086,8 +1090,8 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
       if (Q8) {
         const float2 v = *reinterpret_cast<const float2*>(&scales[1][x & 3][32 * (q >> 3) + 8 * (i >> 2) + 4 * h + (i & 3)]);
         // (a key that the row does not see may have any scale)
-        p0 = whole || p0 > 0.f || p0 != p0 ? p0 * v.x : 0.f;
-        p1 = whole || p1 > 0.f || p1 != p1 ? p1 * v.y : 0.f;
+        p0 = s[q >> 3][i] == -INFINITY ? 0.f : p0 * v.x;
+        p1 = s[q >> 3][i + 1] == -INFINITY ? 0.f : p1 * v.y;
       }
       pw[q] = pack_bf16(p0, p1);
       asm volatile("" : "+v"(pw[q]), "+v"(sum));
@@ -1140,7 +1144,6 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
     // the new scores.
     auto step = [&](int x, f32x16_v (&cur)[2], f32x16_v (&nxt)[2]) __attribute__((always_inline)) {
       const uint32_t bx = x & 1 ? TB : 0, by = TB - bx;
-      const bool whole = is_whole(x);
       const int rr2 = row_of(x + 2);
       uint4 kf[KA][2], vf[VA];
 #pragma unroll
@@ -1161,7 +1164,7 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
         constexpr int g = decltype(G)::value;
 #pragma unroll
         for (int q = 0; q < 16; ++q)
-          if (g == T2 / 16 + q * 11 * T2 / 128) pair(x, whole, q, cur, pw);
+          if (g == T2 / 16 + q * 11 * T2 / 128) pair(x, q, cur, pw);
         // copies over the first three quarters
         constexpr int NG = 2 * NI / NB, STEP = 3 * T2 / 2 / NG;
         if constexpr (g % STEP == STEP / 2 && g / STEP < NG) {
@@ -1231,9 +1234,8 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
     }
     {
       const uint32_t bx = x & 1 ? TB : 0;
-      const bool whole = is_whole(x);
 #pragma unroll
-      for (int q = 0; q < 16; ++q) pair(x, whole, q, sa, pw);
+      for (int q = 0; q < 16; ++q) pair(x, q, sa, pw);
       uint4 vf[VA];
 #pragma unroll
       for (int n = 0; n < VA; ++n) v_load(bx, n, vf);

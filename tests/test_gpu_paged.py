@@ -766,3 +766,29 @@ def test_nan_codes_keep_to_the_rows_that_see_them(dtype, dh, new, length, window
         assert np.isnan(got[see]).all() and np.all((np.abs(got - want) <= tol)[~see])
         for t, old in zip((cache.k, cache.v), kept):
             t.view(torch.uint8)[page, 0, slot] = old
+
+
+@pytest.mark.parametrize("dtype,store", [("bf16", "fp8"), ("bf16", "int8"), ("f32", "fp8"), ("f32", "int8")])
+@pytest.mark.parametrize("dh", [64, 128, 256])
+@pytest.mark.parametrize("new,length", [(1, 130), (6, 43), (70, 200), (70, 1100)])
+def test_nan_scale_of_a_value_that_hardly_counts(dtype, store, dh, new, length):
+    """A value whose scale is NaN makes the rows that see it NaN, also where its probability is 0 in fp32, in a tile
+    that all rows see whole and in one that is masked or cut off."""
+    gen = torch.Generator().manual_seed(dh + length)
+    cu, lens, table, n_pages = pool([new], [length], 16, gen)
+    cache, _, _ = filled(n_pages, 1, 16, dh, store, gen)
+    q = torch.full((new, 2, dh), 4.0, dtype=DT[dtype], device=DEV)
+    b, pos = batch(cu, lens, table), np.arange(length - new, length)
+    for key in (5, length - 1, max(length - 4, length - new)):
+        page, slot = ref.place(table[0], n_pages, 16, key)
+        # q . k = -4 dh 127 * 8 or less, scaled by dh ** -0.5: under -30,000, where the other keys' are above -1,000
+        cache.k.view(torch.uint8)[page, 0, slot] = 0x81 if store == "int8" else 0xFE
+        cache.k_scale[page, 0, slot] = 8.0
+        clean = f64(cache.attend(b, q))
+        assert np.isfinite(clean).all()
+        old = cache.v_scale[page, 0, slot].clone()
+        cache.v_scale[page, 0, slot] = float("nan")
+        got = f64(cache.attend(b, q))
+        cache.v_scale[page, 0, slot] = old
+        assert np.isnan(got[pos >= key]).all()
+        np.testing.assert_array_equal(got[pos < key], clean[pos < key])
