@@ -96,8 +96,10 @@ struct PagedAttnArgs {
   Rows x, o;         // queries, result
   int64_t n_rows;
   int n_q, group;    // query heads, query heads per K/V head
-  float scale2;      // |scale| * log2(e), at least the smallest normal number (a masked -inf stays -inf)
-  int negate;        // scale < 0: queries enter with the other sign
+  // scale * log2(e) = factor * scale2: scale2 > 0 is a normal number (a masked
+  // -inf stays -inf), and factor, by which the queries enter, is 1 or -1, or
+  // 2^-64 of that for a scale that scale2 alone could not hold
+  float scale2, factor;
   int causal, window;
   int nsplit;        // key splits; with more than one, partials go to the workspace
   float* part_o;     // [n_rows * n_q][nsplit][dh]

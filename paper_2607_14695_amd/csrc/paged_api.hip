@@ -230,8 +230,10 @@ int reflex_paged_attention(const reflex_paged_cache* cache, const reflex_paged_b
   a.n_rows = n_rows;
   a.n_q = n_q_heads;
   a.group = n_q_heads / cache->n_kv_heads;
-  a.scale2 = (float)fmax(fabs((double)scale) * 1.4426950408889634, 1.1754943508222875e-38);
-  a.negate = scale < 0.f;
+  const double s2 = fabs((double)scale) * 1.4426950408889634, tiny = 0x1p-126;
+  // (scaled up by 2^64 and then cut off at 2^-126 a score of 2^128 is 2^-62: 0)
+  a.scale2 = (float)(s2 < tiny ? fmax(s2 * 0x1p64, tiny) : s2);
+  a.factor = (scale < 0.f ? -1.f : 1.f) * (s2 < tiny ? 0x1p-64f : 1.f);
   a.causal = causal != 0;
   a.window = window;
   a.nsplit = p.nsplit;

@@ -72,7 +72,7 @@ RFX_DEV void scalar_row(const PagedAttnArgs& a, int64_t row, int head, int b, Sp
   float q[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    q[i] = a.negate ? -to_f(qp[i]) : to_f(qp[i]);
+    q[i] = to_f(qp[i]) * a.factor;
     o[i] = 0.f;
   }
   m = kFloor;
@@ -207,14 +207,17 @@ RFX_DEV uint2 ld_tr8(const unsigned char* lds) {
   return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((RFX_LDS i32x2_v*)lds));
 }
 
-// a fragment, or its negative
-RFX_DEV uint4 signed_frag(uint4 v, int negate, bf16_t) {
-  const uint32_t f = negate ? 0x80008000u : 0u;
-  return make_uint4(v.x ^ f, v.y ^ f, v.z ^ f, v.w ^ f);
-}
-RFX_DEV uint4 signed_frag(uint4 v, int negate, float) {
-  const uint32_t f = negate ? 0x80000000u : 0u;
-  return make_uint4(v.x ^ f, v.y ^ f, v.z ^ f, v.w ^ f);
+// n fragments times a power of two or its negative, mostly 1
+template <int N, typename T> RFX_DEV void scale_frags(uint4 (&v)[N], float factor, T) {
+  if (factor == 1.f) return;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    float x[ElemT<T>::kPerFrag];
+    frag_to_f(v[k], x, T(0));
+#pragma unroll
+    for (int i = 0; i < ElemT<T>::kPerFrag; ++i) x[i] *= factor;
+    v[k] = f_to_frag(x, T(0));
+  }
 }
 
 RFX_DEV uint32_t pack_bf16(float a, float b) {
@@ -459,8 +462,9 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
       if (!Q8) d = QS * k + (QS / 4) * g;
       else if (BF) d = 64 * (k >> 1) + 16 * g + 8 * (k & 1);
       else d = 64 * (k >> 2) + 16 * g + 4 * (k & 3);
-      qf[m][k] = r < t.rows ? signed_frag(ld16(qp + d), a.negate, T(0)) : zero16();
+      qf[m][k] = r < t.rows ? ld16(qp + d) : zero16();
     }
+    scale_frags(qf[m], a.factor, T(0));
   }
   f32x4_v o[MR][NDB];
   float mx[MR], sum[MR];
@@ -891,8 +895,9 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
 #pragma unroll
     for (int k = 0; k < NKS; ++k) {
       const int d = Q8 ? 32 * (k >> 1) + 16 * h + 8 * (k & 1) : 16 * k + 8 * h;
-      qf[k] = r < t.rows ? signed_frag(ld16(qp + d), a.negate, T(0)) : zero16();
+      qf[k] = r < t.rows ? ld16(qp + d) : zero16();
     }
+    scale_frags(qf, a.factor, T(0));
   }
   f32x16_v o[NDB];
 #pragma unroll

@@ -792,3 +792,23 @@ def test_nan_scale_of_a_value_that_hardly_counts(dtype, store, dh, new, length):
         cache.v_scale[page, 0, slot] = old
         assert np.isnan(got[pos >= key]).all()
         np.testing.assert_array_equal(got[pos < key], clean[pos < key])
+
+
+@pytest.mark.parametrize("dtype,store", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "int8")])
+@pytest.mark.parametrize("new,length", [(1, 3), (3, 12), (70, 90)])
+@pytest.mark.parametrize("scale", [0.0, 4e-39, -4e-39, 1e-42])
+def test_scales_under_the_normal_numbers(dtype, store, new, length, scale):
+    """Scales next to zero against products of up to 2^127: their share of the scores, and no more."""
+    gen = torch.Generator().manual_seed(41)
+    cu, lens, table, n_pages = pool([new], [length], 16, gen)
+    cache, k, v = filled(n_pages, 1, 16, 64, store, gen)
+    up = 2.0 ** 60
+    if store == "int8":
+        cache.k_scale *= up
+    else:
+        cache.k.mul_(up)
+    q = (draw(gen, (new, 2, 64), "bf16").float() * 2.0 ** 58).to(DT[dtype])
+    got = f64(cache.attend(batch(cu, lens, table), q.to(DEV), scale=scale))
+    # (the scale as the call takes it, rounded to fp32)
+    want, tol = attend_ref(q, k * up, v, cu, lens, table, 0, dtype, scale=float(np.float32(scale)))
+    assert np.all(np.abs(got - want) <= tol)
