@@ -619,6 +619,7 @@ int reflex_paged_read(const reflex_paged_cache* cache, const reflex_paged_batch*
  * the sequence's length, these are the present tokens j < L, with causal != 0
  * only j <= p, and with window > 0 only j > p - window.  A row that sees none
  * gets zeros, and so does one all of whose scores are below -2e38.
+ * scale * log2(e) is finite in fp32.
  * Keys that a row does not see have no part in its result, whatever they hold
  * (NaN and infinities included).  Probabilities enter the second product
  * rounded to dtype or finer, all sums are fp32; equal calls give equal bits.

@@ -2,6 +2,7 @@
 // the host-visible arguments, then one or two launches on the caller's stream.
 // What lies in device memory (row offsets, lengths, page table) is checked by
 // the kernels, entry by entry, where they use it.
+#include <float.h>
 #include <math.h>
 #include <string.h>
 
@@ -218,7 +219,8 @@ int reflex_paged_attention(const reflex_paged_cache* cache, const reflex_paged_b
   RFX_CHECK(reflex_paged_attention_workspace(cache, batch, n_rows, n_q_heads, dtype, &need));
   RFX_CHECK(check_rows(q, n_rows, dtype));
   RFX_CHECK(check_rows(out, n_rows, dtype));
-  if (!isfinite(scale) || window < 0) return REFLEX_EINVAL;
+  const double s2 = fabs((double)scale) * 1.4426950408889634;
+  if (!(s2 <= (double)FLT_MAX) || window < 0) return REFLEX_EINVAL;
   if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return REFLEX_EINVAL;
   if (n_rows == 0 || batch->n_seqs == 0) return REFLEX_OK;
   const PagedAttnPlan p = paged_attention_plan(*cache, *batch, n_rows, n_q_heads, dtype, window);
@@ -230,7 +232,7 @@ int reflex_paged_attention(const reflex_paged_cache* cache, const reflex_paged_b
   a.n_rows = n_rows;
   a.n_q = n_q_heads;
   a.group = n_q_heads / cache->n_kv_heads;
-  const double s2 = fabs((double)scale) * 1.4426950408889634, tiny = 0x1p-126;
+  const double tiny = 0x1p-126;
   // (scaled up by 2^64 and then cut off at 2^-126 a score of 2^128 is 2^-62: 0)
   a.scale2 = (float)(s2 < tiny ? fmax(s2 * 0x1p64, tiny) : s2);
   a.factor = (scale < 0.f ? -1.f : 1.f) * (s2 < tiny ? 0x1p-64f : 1.f);

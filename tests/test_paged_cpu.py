@@ -208,3 +208,11 @@ def test_reference_quantiser_on_known_values():
     assert np.isnan(ref.encode_row(np.array([1.0, np.inf]), "int8")[1])
     v, s = ref.encode_row(np.zeros(4), "fp8")
     assert s == 2.0 ** -126 and not v.any()
+
+
+def test_scales_past_fp32_are_refused():
+    """The scale enters the exponent times log2(e), which has to be finite in fp32 too."""
+    for scale in (2.4e38, 3.4e38, -3.4e38):
+        assert attend(n=0, scale=scale) == R.REFLEX_EINVAL
+    for scale in (2.3e38, -2.3e38, 0.0, 1e-45):
+        assert attend(n=0, scale=scale) == R.REFLEX_OK
