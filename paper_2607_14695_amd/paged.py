@@ -3,7 +3,8 @@ attention of a chunk of new tokens over it (include/reflex.h, "Backbone operator
 
 Argument marshalling only, as in ``reflex.py``: every operator runs in the library's HIP kernels on the caller's
 current stream of the tensors' device, and nothing waits for the GPU.  The operators record no gradients: a tensor
-that needs one is refused (``Rotary.apply(..., inverse=True)`` is the rotation's gradient).
+that needs one or carries a tangent is refused, by calls and as pages of a cache (``Rotary.apply(..., inverse=True)``
+is the rotation's gradient).
 """
 from __future__ import annotations
 
@@ -11,6 +12,7 @@ import ctypes
 from typing import Optional, Sequence, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 from .reflex import (DTYPE_BF16, DTYPE_F32, STORE_BF16, STORE_F32, STORE_FP8, STORE_INT8, LADDERS, PagedBatchC,
                      PagedCacheC, RotaryC, RowsC, _check, load_library)
@@ -21,14 +23,27 @@ _STORES = {torch.float32: STORE_F32, torch.bfloat16: STORE_BF16, torch.float8_e4
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
 
+def _dual_level() -> bool:
+    """Whether forward-mode differentiation is on (if torch does not say, tensors are asked, half a microsecond each)."""
+    return getattr(forward_ad, "_current_level", 0) >= 0
+
+
+def _no_gradient(x: torch.Tensor, what: str) -> None:
+    """Refuse a tensor of which a gradient, or a tangent of forward-mode differentiation, would be dropped."""
+    if x.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{what} needs a gradient, which these operators do not record")
+    if _dual_level() and forward_ad.unpack_dual(x).tangent is not None:
+        raise ValueError(f"{what} carries a tangent, and these operators compute no gradient of either mode")
+
+
 def _rows(x: torch.Tensor, n: int, heads: int, head_dim: int, device: torch.device, what: str) -> RowsC:
     """The C view of [n][heads][head_dim]; a dimension of one element may have any stride."""
     if x.shape != (n, heads, head_dim):
         raise ValueError(f"{what} is [{n}, {heads}, {head_dim}], got {tuple(x.shape)}")
     if x.device != device:
         raise ValueError(f"{what} is on {x.device}, not on {device}")
-    if x.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{what} needs a gradient, which these operators do not record")
+    if x.requires_grad or _dual_level():
+        _no_gradient(x, what)
     rs, hs, es = x.stride()
     if es != 1:
         raise ValueError(f"{what} needs contiguous heads")
@@ -143,6 +158,10 @@ class PagedCache:
         if scaled != (k_scale is not None) or scaled != (v_scale is not None):
             raise ValueError("8-bit pages have scales, others none")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        for what, t in (("k", k), ("v", v), ("k_scale", k_scale), ("v_scale", v_scale)):
+            if t is not None:
+                with torch.enable_grad():  # (the cache outlives a no_grad block that it is made in)
+                    _no_gradient(t, what)
         self.c = PagedCacheC(
             _index(k, k.shape, k.dtype, "k"), _index(v, k.shape, k.dtype, "v", k.device),
             _index(k_scale, k.shape[:3], torch.float32, "k_scale", k.device) if scaled else None,

@@ -12,6 +12,7 @@ Tolerances.  One rounding to a type is off by at most half a step: 2^-8 of the v
 import numpy as np
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 from paper_2607_14695_amd import reflex as R
 from paper_2607_14695_amd import workloads as WL
@@ -812,3 +813,28 @@ def test_scales_under_the_normal_numbers(dtype, store, new, length, scale):
     # (the scale as the call takes it, rounded to fp32)
     want, tol = attend_ref(q, k * up, v, cu, lens, table, 0, dtype, scale=float(np.float32(scale)))
     assert np.all(np.abs(got - want) <= tol)
+
+
+def test_gradients_that_would_be_dropped_are_refused():
+    """Pages that need a gradient, whatever mode the cache is made in, and tangents of forward-mode differentiation on
+    pages or rows."""
+    gen = torch.Generator().manual_seed(1)
+    cu, lens, table, n_pages = pool([2], [20], 16, gen)
+    b = batch(cu, lens, table)
+    x = torch.zeros(2, 2, 64, device=DEV)
+    for name, dtype in (("k", torch.float32), ("v", torch.float32), ("k_scale", torch.int8), ("v_scale", torch.int8)):
+        cache = PagedCache.zeros(n_pages, 16, 2, 64, dtype)
+        held = {m: getattr(cache, m) for m in ("k", "v", "k_scale", "v_scale")}
+        with torch.no_grad(), pytest.raises(ValueError, match=f"{name} needs a gradient"):
+            PagedCache(**{**held, name: held[name].clone().requires_grad_()})
+        PagedCache(**held)
+        with forward_ad.dual_level(), pytest.raises(ValueError, match=f"{name} carries a tangent"):
+            PagedCache(**{**held, name: forward_ad.make_dual(held[name], torch.ones_like(held[name]))})
+    cache = PagedCache.zeros(n_pages, 16, 2, 64, torch.float32)
+    with forward_ad.dual_level():
+        d = forward_ad.make_dual(x, torch.ones_like(x))
+        for call in (lambda: cache.write(b, d, x), lambda: cache.write(b, x, d), lambda: cache.attend(b, d),
+                     lambda: cache.attend(b, x, out=d), lambda: cache.read(b, 2, out=(x, d))):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+        cache.attend(b, x)

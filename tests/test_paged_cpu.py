@@ -6,6 +6,7 @@ import subprocess
 import numpy as np
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 from paper_2607_14695_amd import reflex as R
 from paper_2607_14695_amd.paged import PagedBatch, PagedCache, Rotary
@@ -216,3 +217,15 @@ def test_scales_past_fp32_are_refused():
         assert attend(n=0, scale=scale) == R.REFLEX_EINVAL
     for scale in (2.3e38, -2.3e38, 0.0, 1e-45):
         assert attend(n=0, scale=scale) == R.REFLEX_OK
+
+
+def test_tangents_are_refused():
+    """Forward-mode differentiation: a tangent would be dropped without a word, with gradients recorded or not."""
+    rot, pos, x = Rotary(64), torch.zeros(4, dtype=torch.int64), torch.zeros(4, 2, 64)
+    with forward_ad.dual_level():
+        d = forward_ad.make_dual(x, torch.ones_like(x))
+        for call in (lambda: rot.apply(d, pos), lambda: rot.apply(x, pos, out=d)):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+            with torch.no_grad(), pytest.raises(ValueError, match="tangent"):
+                call()
