@@ -23,8 +23,15 @@ _STORES = {torch.float32: STORE_F32, torch.bfloat16: STORE_BF16, torch.float8_e4
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
 
+def _int32(x: int, what: str) -> int:
+    """ctypes would cut an integer to its low 32 bits."""
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{what} {x} does not fit 32 bits")
+    return x
+
+
 def _dual_level() -> bool:
-    """Whether forward-mode differentiation is on (if torch does not say, tensors are asked, half a microsecond each)."""
+    """Whether forward-mode differentiation is on (if torch does not say, every tensor is asked)."""
     return getattr(forward_ad, "_current_level", 0) >= 0
 
 
@@ -88,7 +95,8 @@ class Rotary:
                  ladder: str = "shared"):
         if ladder not in LADDERS:
             raise ValueError(f"unknown ladder {ladder!r}")
-        sections = [head_dim // 2] if sections is None else [int(s) for s in sections]
+        _int32(head_dim, "head_dim")
+        sections = [head_dim // 2] if sections is None else [_int32(int(s), "sections:") for s in sections]
         self.lib = load_library()
         self.head_dim, self.sections, self.theta, self.ladder = head_dim, sections, theta, ladder
         self.c = RotaryC()
@@ -133,6 +141,7 @@ class PagedBatch:
     def __init__(self, cu_rows: torch.Tensor, lengths: torch.Tensor, page_table: torch.Tensor, max_length: int = 0):
         if lengths.dim() != 1 or page_table.dim() != 2:
             raise ValueError("lengths is [sequences] and page_table [sequences, pages]")
+        _int32(max_length, "max_length")
         n = lengths.shape[0]
         self.device = lengths.device
         self.tensors = (cu_rows, lengths, page_table)
@@ -228,6 +237,7 @@ class PagedCache:
             raise ValueError(f"q is [rows, heads, head_dim], got {tuple(q.shape)}")
         n, heads, dh = q.shape
         dt = _dtype(q.dtype)
+        _int32(window, "window")
         qr = _rows(q, n, heads, self.head_dim, self.device, "q")
         if out is None:
             out = torch.empty((n, heads, dh), dtype=q.dtype, device=self.device)

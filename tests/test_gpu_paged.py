@@ -838,3 +838,13 @@ def test_gradients_that_would_be_dropped_are_refused():
             with pytest.raises(ValueError, match="tangent"):
                 call()
         cache.attend(b, x)
+
+
+def test_windows_that_do_not_fit_are_refused():
+    gen = torch.Generator().manual_seed(1)
+    cu, lens, table, n_pages = pool([2], [20], 16, gen)
+    cache, b = PagedCache.zeros(n_pages, 16, 2, 64, torch.float32), batch(cu, lens, table)
+    x = torch.zeros(2, 2, 64, device=DEV)
+    for window in (2 ** 31, 2 ** 32, 2 ** 32 + 5, -2 ** 31 - 1):
+        with pytest.raises(ValueError, match="window"):
+            cache.attend(b, x, window=window)

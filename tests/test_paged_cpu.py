@@ -229,3 +229,15 @@ def test_tangents_are_refused():
                 call()
             with torch.no_grad(), pytest.raises(ValueError, match="tangent"):
                 call()
+
+
+def test_integers_that_do_not_fit_are_refused():
+    """Python's integers are not cut to 32 bits on their way into the C structs."""
+    with pytest.raises(ValueError, match="sections"):
+        Rotary(64, (2 ** 32 + 32,))
+    with pytest.raises(ValueError, match="head_dim"):
+        Rotary(2 ** 32 + 64, (32,))
+    t32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    for length in (2 ** 32, 2 ** 32 + 5, -2 ** 32):
+        with pytest.raises(ValueError, match="max_length"):
+            PagedBatch(t32(3), t32(2), t32(2, 4), length)
