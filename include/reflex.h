@@ -572,7 +572,9 @@ typedef struct reflex_paged_cache {
  * A table entry outside [0, n_pages), and every token beyond max_pages pages
  * or before the sequence's start, is absent: nothing is written for it, it
  * reads as zeros and no query sees it.  Sequences may share pages that a call
- * only reads; of two rows of one write for the same slot either may win.
+ * only reads.  No two rows of one write may be for the same slot unless their
+ * values (and positions) are equal: what the slot holds then is undefined, and
+ * may be codes, a scale, K and V of different rows.
  * cu_rows is non-decreasing from a value >= 0; what exceeds the call's n_rows
  * is cut off there.
  * max_length: the length that the longest sequence is expected to reach (0:

@@ -197,7 +197,8 @@ class PagedCache:
     def write(self, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor, rotary: Optional[Rotary] = None,
               positions: Optional[torch.Tensor] = None) -> None:
         """Write the batch's rows k, v [rows, kv heads, head dim] into their pages, the keys rotated first where a
-        plan is given: by ``positions``, or by each token's index in its sequence."""
+        plan is given: by ``positions``, or by each token's index in its sequence.  Rows for the same slot (sequences
+        that share the page) have to be equal."""
         n = k.shape[0]
         if v.dtype != k.dtype:
             raise ValueError("k and v have one type")

@@ -848,3 +848,31 @@ def test_windows_that_do_not_fit_are_refused():
     for window in (2 ** 31, 2 ** 32, 2 ** 32 + 5, -2 ** 31 - 1):
         with pytest.raises(ValueError, match="window"):
             cache.attend(b, x, window=window)
+
+
+@pytest.mark.parametrize("dtype,store", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "int8")])
+def test_rows_for_the_same_slot(dtype, store):
+    """Sequences that share their prefix's pages and write them in one call: equal rows leave what one of them would;
+    rows that differ leave every other slot as it should be."""
+    gen = torch.Generator().manual_seed(43)
+    n, ps, dh = 40, 8, 128
+    cu, lens, table, n_pages = pool([n, n, n], [n, n, n], ps, gen)
+    shared = 16
+    table[1:, :shared // ps] = table[0, :shared // ps]
+    k, v = (draw(gen, (3, n, 2, dh), dtype) for _ in range(2))
+    k[1:, :shared], v[1:, :shared] = k[0, :shared], v[0, :shared]
+    rot = Rotary(dh)
+    one, two = (PagedCache.zeros(n_pages, ps, 2, dh, CODE[store]) for _ in range(2))
+    b = batch(cu, lens, table)
+    one.write(b, k.view(-1, 2, dh).to(DEV), v.view(-1, 2, dh).to(DEV), rotary=rot)
+    for s in range(3):  # the same one sequence at a time
+        two.write(batch(cu[:2], lens[:1], table[s:s + 1]), k[s].to(DEV), v[s].to(DEV), rotary=rot)
+    names = ("k", "v", "k_scale", "v_scale") if one.k_scale is not None else ("k", "v")
+    for m in names:
+        assert torch.equal(getattr(one, m).view(torch.uint8), getattr(two, m).view(torch.uint8))
+    k[1, :shared] += 1
+    one.write(b, k.view(-1, 2, dh).to(DEV), v.view(-1, 2, dh).to(DEV), rotary=rot)
+    kept = torch.ones(n_pages, dtype=torch.bool)
+    kept[table[0, :shared // ps].long()] = False
+    for m in names:
+        assert torch.equal(getattr(one, m).cpu()[kept].view(torch.uint8), getattr(two, m).cpu()[kept].view(torch.uint8))
