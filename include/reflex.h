@@ -469,8 +469,8 @@ int reflex_profile_graph(reflex_ctx* ctx, const float* state, const float* noise
  * several threads may make them at once.
  *
  * Element types: `dtype` (REFLEX_DTYPE_*) is the type of queries, keys, values
- * and results outside the cache.  All arithmetic is fp32 or wider; results are
- * rounded once.
+ * and results outside the cache.  Arithmetic is fp32 or wider and results are
+ * rounded once; only the attention rounds before that, its probabilities.
  */
 
 /* Packed rows of heads: element (row r, head h, d) at data[r*row_stride +
@@ -536,7 +536,8 @@ int reflex_rotary_apply(const reflex_rotary* plan, const int64_t* positions, int
  *         448 * scale, code = x / scale to nearest.
  * Ties go to the even code.  What lies next to a border is decided exactly: K
  * is rotated and divided in 64 bits.  A row with an infinity or a NaN gets the
- * scale NaN: all of it reads as NaN. */
+ * scale NaN: all of it reads as NaN.  Pages that a caller fills may hold any
+ * codes, and scales that are finite or NaN. */
 #define REFLEX_STORE_F32 0
 #define REFLEX_STORE_BF16 1
 #define REFLEX_STORE_FP8 2
@@ -624,7 +625,9 @@ int reflex_paged_read(const reflex_paged_cache* cache, const reflex_paged_batch*
  * scale * log2(e) is finite in fp32.
  * Keys that a row does not see have no part in its result, whatever they hold
  * (NaN and infinities included).  Probabilities enter the second product
- * rounded to dtype or finer, all sums are fp32; equal calls give equal bits.
+ * rounded to dtype or finer (in bf16 to 8 bits, with few rows to 16), all sums
+ * are fp32; equal calls give equal bits.  The sums are divided last: values up
+ * to V over L keys need 2^8 L V to be finite in fp32.
  * q, out: [n_rows][n_q_heads][head_dim], not overlapping.  n_q_heads: a
  * multiple of n_kv_heads; n_rows * n_q_heads <= 2^23.
  * workspace: at least the bytes that reflex_paged_attention_workspace gives
