@@ -9,6 +9,8 @@ Tolerances.  One rounding to a type is off by at most half a step: 2^-8 of the v
   probability is rounded once (2^-8).  All of it weighs on `spread` = sum p|v|, and the sum of the probabilities
   doubles it.  Then the result's own rounding.
 """
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -876,3 +878,62 @@ def test_rows_for_the_same_slot(dtype, store):
     kept[table[0, :shared // ps].long()] = False
     for m in names:
         assert torch.equal(getattr(one, m).cpu()[kept].view(torch.uint8), getattr(two, m).cpu()[kept].view(torch.uint8))
+
+
+@pytest.mark.parametrize("store", ["bf16", "fp8", "int8"])
+@pytest.mark.parametrize("dh", [64, 128, 256])
+def test_probabilities_of_few_rows_keep_sixteen_bits(store, dh):
+    """With few rows the probabilities enter the second product as two bf16 halves, 2^-16 of each.  Here the value of
+    the largest one cancels the others', so that the result's own rounding hides nothing."""
+    gen = torch.Generator().manual_seed(dh)
+    seqs = [2, 5, 33, 64, 200]
+    cu, lens, table, n_pages = pool([1] * len(seqs), seqs, 16, gen)
+    cache, k, v = filled(n_pages, 1, 16, dh, store, gen)
+    q = draw(gen, (len(seqs), 1, dh), "bf16") * 0.25
+    for b, n in enumerate(seqs):
+        pg, sl = np.array([ref.place(table[b], n_pages, 16, j) for j in range(n)]).T
+        p = np.exp(dh ** -0.5 * (k[pg, 0, sl] @ f64(q)[b, 0]))
+        top = int(np.argmax(p))
+        rest = -(np.delete(p, top) @ np.delete(v[pg, 0, sl], top, 0)) / p[top]
+        at = pg[top], 0, sl[top]
+        if store == "bf16":
+            cache.v[at] = torch.from_numpy(rest).to(torch.bfloat16).to(DEV)
+            v[at] = f64(cache.v[at])
+        else:
+            code, scale = ref.encode_row(np.float64(np.float32(rest)), store)
+            cache.v[at] = torch.from_numpy(code).float().to(CODE[store]).to(DEV)
+            cache.v_scale[at] = float(scale)
+            v[at] = code * scale
+    got = f64(cache.attend(batch(cu, lens, table), q.to(DEV)))
+    want, tol = attend_ref(q, k, v, cu, lens, table, 0, "bf16", prob=2.0 ** -16)
+    assert np.all(np.abs(got - want) <= tol)
+
+
+@pytest.mark.parametrize("dtype,store,dh", [("bf16", "bf16", 128), ("bf16", "int8", 256), ("f32", "f32", 64)])
+@pytest.mark.parametrize("new", [1, 60])
+def test_workspace_holds_every_window(dtype, store, dh, new):
+    """The workspace query knows no window: a call with any uses no more than it reports, and asks for no less."""
+    gen = torch.Generator().manual_seed(23)
+    cu, lens, table, n_pages = pool([new, new], [3000, 700], 16, gen)
+    cache, k, v = filled(n_pages, 1, 16, dh, store, gen)
+    q = draw(gen, (2 * new, 2, dh), dtype).to(DEV)
+    b = batch(cu, lens, table)
+    lib, need = R.load_library(), ctypes.c_size_t(0)
+    code = R.DTYPE_BF16 if dtype == "bf16" else R.DTYPE_F32
+    assert lib.reflex_paged_attention_workspace(cache._ref, b._ref, 2 * new, 2, code, ctypes.byref(need)) == R.REFLEX_OK
+    assert need.value > 0
+    ws = torch.empty(need.value + 4096, dtype=torch.uint8, device=DEV)
+    assert ws.data_ptr() % 256 == 0
+    qr = R.RowsC(q.data_ptr(), 2 * dh, dh)
+    for window in (0, 1, 63, 128, 129, 500, 1025, 2999, 2 ** 31 - 1):
+        ws.fill_(0xA5)
+        out = torch.empty_like(q)
+        yr = R.RowsC(out.data_ptr(), 2 * dh, dh)
+        call = lambda nb: lib.reflex_paged_attention(  # noqa: E731
+            cache._ref, b._ref, ctypes.byref(qr), ctypes.byref(yr), 2 * new, 2, code, dh ** -0.5, 1, window,
+            ws.data_ptr(), nb, torch.cuda.current_stream().cuda_stream)
+        assert call(need.value - 1) == R.REFLEX_EINVAL
+        assert call(need.value) == R.REFLEX_OK
+        torch.cuda.synchronize()
+        assert bool((ws[need.value:] == 0xA5).all())
+        assert torch.equal(out, cache.attend(b, q, window=window))

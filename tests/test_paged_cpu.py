@@ -241,3 +241,21 @@ def test_integers_that_do_not_fit_are_refused():
     for length in (2 ** 32, 2 ** 32 + 5, -2 ** 32):
         with pytest.raises(ValueError, match="max_length"):
             PagedBatch(t32(3), t32(2), t32(2, 4), length)
+
+
+@pytest.mark.parametrize("rows,heads,dtype,store,max_length,splits", [
+    # 128 keys at least to a split, at most 64 splits
+    (1, 4, R.DTYPE_BF16, R.STORE_BF16, 128, 1), (1, 4, R.DTYPE_BF16, R.STORE_BF16, 129, 2),
+    (1, 4, R.DTYPE_BF16, R.STORE_BF16, 8192, 64), (1, 4, R.DTYPE_BF16, R.STORE_BF16, 8193, 33),
+    (1, 4, R.DTYPE_BF16, R.STORE_BF16, 0, 64), (1, 4, R.DTYPE_F32, R.STORE_F32, 16384, 64),
+    # 4,096 rows of two heads on each of two K/V heads: 128 tiles of 128 rows, or 512 of 32 in fp32; 512 workgroups
+    (4096, 4, R.DTYPE_BF16, R.STORE_BF16, 0, 4), (4096, 4, R.DTYPE_F32, R.STORE_F32, 0, 1),
+    (4096, 4, R.DTYPE_BF16, R.STORE_INT8, 500, 4), (4096, 4, R.DTYPE_BF16, R.STORE_INT8, 300, 3)])
+def test_workspace_bytes(rows, heads, dtype, store, max_length, splits):
+    """Exactly the partial sums (head_dim and two fp32 a row, head and split) of the splits that a call makes.  A longer
+    memory may need less: 64 splits of 128 keys hold 8,192, and 8,193 take 33 of 256."""
+    need, b = ctypes.c_size_t(0), ctypes.byref
+    scales = dict(k_scale=A, v_scale=A) if store == R.STORE_INT8 else {}
+    c, q = cache_c(n_pages=4096, store=store, **scales), batch_c(max_pages=1024, n_seqs=1, max_length=max_length)
+    assert R.load_library().reflex_paged_attention_workspace(b(c), b(q), rows, heads, dtype, b(need)) == R.REFLEX_OK
+    assert need.value == (0 if splits == 1 else rows * heads * splits * (64 + 2) * 4)
