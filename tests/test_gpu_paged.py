@@ -937,3 +937,35 @@ def test_workspace_holds_every_window(dtype, store, dh, new):
         torch.cuda.synchronize()
         assert bool((ws[need.value:] == 0xA5).all())
         assert torch.equal(out, cache.attend(b, q, window=window))
+
+
+@pytest.mark.parametrize("dtype,store", [("bf16", "bf16"), ("f32", "int8")])
+@pytest.mark.parametrize("cu,n", [([0, 5, 12], 8), ([3, 100, 300], 160), ([0, 1, 2], 1), ([9, 9, 12], 7)])
+def test_rows_past_the_call_are_cut_off(dtype, store, cu, n):
+    """Row offsets that run past the call's rows: the rows that it has keep their tokens, in all three calls."""
+    gen = torch.Generator().manual_seed(n)
+    hk, ps, dh = 2, 16, 64
+    _, lens, table, n_pages = pool([0, 0], [130, 260], ps, gen)
+    cu = torch.tensor(cu, dtype=torch.int32)
+    cache, k, v = filled(n_pages, hk, ps, dh, store, gen)
+    q = draw(gen, (n, 4, dh), dtype)
+    out = torch.full((n, 4, dh), 77.0, dtype=DT[dtype], device=DEV)
+    check_attention(q, cache, (k, v), cu, lens, table, True, 0, dtype, out=out)
+    own = torch.arange(n) >= int(cu[0])
+    assert bool((out.cpu()[~own] == 77).all())
+    b = batch(cu, lens, table)
+    rk, rv = (torch.full((n, hk, dh), 77.0, dtype=DT[dtype], device=DEV) for _ in range(2))
+    cache.read(b, n, out=(rk, rv))
+    want = np.full((n, hk, dh), 77.0)
+    new = torch.randn(n, hk, dh, generator=gen).to(DT[dtype]).to(DEV)
+    old = cache.k.view(torch.uint8).cpu().clone()
+    cache.write(b, new, new)
+    changed = (cache.k.view(torch.uint8).cpu() != old).any(-1).any(1).numpy()
+    rows = np.zeros((n_pages, ps), dtype=bool)
+    for r, s, p in ref.rows_of(cu, lens):
+        if r < n:
+            at = ref.place(table[s], n_pages, ps, p)
+            want[r] = k[at[0], :, at[1]]
+            rows[at] = True
+    assert np.array_equal(f64(rk), f64(torch.from_numpy(want).float().to(DT[dtype])))
+    np.testing.assert_array_equal(changed, rows)
