@@ -72,61 +72,6 @@ RFX_DEV void turns_of(const reflex_rotary& plan, const int64_t* pos, int64_t ps,
   }
 }
 
-// ---------------------------------------------------------------------------
-// rotary
-// ---------------------------------------------------------------------------
-// 24,576 rows of 8 heads of 256 in fp32 (403 MB read and written) take 86 us,
-// 4.7 TB/s, where a large copy reaches 4.9; 768 rows in bf16 5 us and eight rows
-// 4 us, the latency of positions, frequencies and rows.
-template <typename T>
-__global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
-  const int G = a.plan.head_dim >> 4;
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = t / G;
-  const int g = (int)(t - row * G);
-  if (row >= a.n_rows) return;
-  const int half = a.plan.head_dim >> 1;
-  const int h0 = blockIdx.y * a.heads_per, h1 = min(a.n_heads, h0 + a.heads_per);
-  const T* x = reinterpret_cast<const T*>(a.x.p) + row * a.x.rs + 8 * g;
-  T* y = reinterpret_cast<T*>(const_cast<char*>(a.y.p)) + row * a.y.rs + 8 * g;
-  double f[8];
-  turns_of(a.plan, a.pos, a.ps, row, 0, g, f);
-  float cs[8], sn[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    sincospif(2.f * (float)f[i], &sn[i], &cs[i]);
-    if (a.inverse) sn[i] = -sn[i];
-  }
-  for (int h = h0; h < h1; ++h) {
-    float u[8], w[8], p[8], q[8];
-    ld8(x + h * a.x.hs, u);
-    ld8(x + h * a.x.hs + half, w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = u[i] * cs[i] - w[i] * sn[i];
-      q[i] = w[i] * cs[i] + u[i] * sn[i];
-    }
-    st8(y + h * a.y.hs, p);
-    st8(y + h * a.y.hs + half, q);
-  }
-}
-
-// ---------------------------------------------------------------------------
-// paged write
-// ---------------------------------------------------------------------------
-// Nearest fp32 to x whose rounding to fewer bits is that of x itself: where
-// the conversion is inexact the last bit is set (rounding to odd).
-RFX_DEV float odd_float(double x) {
-  float f = (float)x;
-  const double d = (double)f;
-  if (d != x) {
-    uint32_t u = __float_as_uint(f);
-    if (fabs(d) > fabs(x)) u -= 1;
-    f = __uint_as_float(u | 1u);
-  }
-  return f;
-}
-
 // Sine and cosine of a fraction of a turn in [-1/2, 1/2]: the
 // nearest quarter turn is taken off, and the Taylor series of both functions
 // (sine to x^15, cosine to x^14) hold the rest, |x| <= pi / 4, to 2^-49 of 1.
@@ -157,6 +102,75 @@ RFX_DEV void sincos_turn(double f, double* sn, double* cs) {
   };
   *sn = flip(a, n);
   *cs = flip(b, n + 1);
+}
+
+// The same for values of type T, in fp32: rounded from 64 bits for fp32 values (a
+// fraction rounded to fp32 first is off by 2^-26 of a turn, all of a small sine
+// next to half a turn), from an fp32 fraction for bf16 ones.
+template <typename T> RFX_DEV void sincos_for(double f, float* sn, float* cs) {
+  if constexpr (sizeof(T) == 4) {
+    double s, c;
+    sincos_turn(f, &s, &c);
+    *sn = (float)s;
+    *cs = (float)c;
+  } else {
+    sincospif(2.f * (float)f, sn, cs);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// rotary
+// ---------------------------------------------------------------------------
+// 24,576 rows of 8 heads of 256 in fp32 (403 MB read and written) take 86 us,
+// 4.7 TB/s, where a large copy reaches 4.9; 768 rows in bf16 5 us and eight rows
+// 4 us, the latency of positions, frequencies and rows.
+template <typename T>
+__global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
+  const int G = a.plan.head_dim >> 4;
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = t / G;
+  const int g = (int)(t - row * G);
+  if (row >= a.n_rows) return;
+  const int half = a.plan.head_dim >> 1;
+  const int h0 = blockIdx.y * a.heads_per, h1 = min(a.n_heads, h0 + a.heads_per);
+  const T* x = reinterpret_cast<const T*>(a.x.p) + row * a.x.rs + 8 * g;
+  T* y = reinterpret_cast<T*>(const_cast<char*>(a.y.p)) + row * a.y.rs + 8 * g;
+  double f[8];
+  turns_of(a.plan, a.pos, a.ps, row, 0, g, f);
+  float cs[8], sn[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    sincos_for<T>(f[i], &sn[i], &cs[i]);
+    if (a.inverse) sn[i] = -sn[i];
+  }
+  for (int h = h0; h < h1; ++h) {
+    float u[8], w[8], p[8], q[8];
+    ld8(x + h * a.x.hs, u);
+    ld8(x + h * a.x.hs + half, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[i] = u[i] * cs[i] - w[i] * sn[i];
+      q[i] = w[i] * cs[i] + u[i] * sn[i];
+    }
+    st8(y + h * a.y.hs, p);
+    st8(y + h * a.y.hs + half, q);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// paged write
+// ---------------------------------------------------------------------------
+// Nearest fp32 to x whose rounding to fewer bits is that of x itself: where
+// the conversion is inexact the last bit is set (rounding to odd).
+RFX_DEV float odd_float(double x) {
+  float f = (float)x;
+  const double d = (double)f;
+  if (d != x) {
+    uint32_t u = __float_as_uint(f);
+    if (fabs(d) > fabs(x)) u -= 1;
+    f = __uint_as_float(u | 1u);
+  }
+  return f;
 }
 
 // Scale of a row from the bits of its largest magnitude; NaN for a row with a
@@ -298,7 +312,7 @@ __global__ __launch_bounds__(256) void paged_write_kernel(const PagedWriteArgs a
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if constexpr (Q) sincos_turn(f[i], &sn[i], &cs[i]);
-      else sincospif(2.f * (float)f[i], &sn[i], &cs[i]);
+      else sincos_for<T>(f[i], &sn[i], &cs[i]);
     }
   } else {
 #pragma unroll

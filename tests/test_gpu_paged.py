@@ -969,3 +969,27 @@ def test_rows_past_the_call_are_cut_off(dtype, store, cu, n):
             rows[at] = True
     assert np.array_equal(f64(rk), f64(torch.from_numpy(want).float().to(DT[dtype])))
     np.testing.assert_array_equal(changed, rows)
+
+
+@pytest.mark.parametrize("through", ["apply", "write"])
+def test_small_sines_of_fp32(through):
+    """Next to whole and half turns the sine is small and keeps its bits.  With x = 0 in the first half a result is one
+    product: the sine's or the cosine's rounding and its own, 2^-23 of it; the angle's 64 bits leave 2^-52 of it, the
+    series 2^-49 of the sine's quarter turn."""
+    pos = torch.tensor([0, 1, 3, 22, 355, 710, 103993, 104348, 833719, 10 ** 6], dtype=torch.int64)
+    n, dh = len(pos), 64
+    x = torch.zeros(n, 1, dh)
+    x[..., dh // 2:] = 1.0 + torch.rand(n, 1, dh // 2, generator=torch.Generator().manual_seed(3))
+    rot = Rotary(dh)
+    ang = ref.rotary_angles(pos.numpy(), (dh // 2,), 10000.0, "shared", dh // 2)
+    want = ref.rotate(f64(x), ang)
+    if through == "apply":
+        got = f64(rot.apply(x.to(DEV), pos.to(DEV)))
+    else:
+        cache = PagedCache.zeros(1, 16, 1, dh, torch.float32)
+        b = batch(*[torch.tensor(t, dtype=torch.int32) for t in ([0, n], [n], [[0]])])
+        cache.write(b, x.to(DEV), x.to(DEV), rotary=rot, positions=pos.to(DEV))
+        got = f64(cache.read(b, n, torch.float32)[0])
+    # (the angle in turns has steps of 2^-53 of the angle, which is up to 10^6)
+    tol = 2.0 ** -23 * np.abs(want) + 2 * (2.0 ** -49 + 4 * 2.0 ** -53 * np.concatenate([ang, ang], 1)[:, None])
+    assert np.all(np.abs(got - want) <= tol)
