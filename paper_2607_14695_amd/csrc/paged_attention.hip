@@ -40,8 +40,8 @@ RFX_DEV Span span_of(const PagedAttnArgs& a, int pos, int len) {
 // The keys of split `split` of a tile that sees [lo, hi): equal runs of whole
 // 128s, so that a window, a causal mask or a short sequence leaves no split
 // without work before the others are down to 128.  (64 single tokens with a
-// window of 1,024 over 15,409 keys 29 us, where equal runs of the longest
-// sequence took 42.)
+// window of 1,024 over 15,409 keys took 29 us, where equal runs of the longest
+// sequence took 42; now 26.)
 RFX_DEV Span split_of(const PagedAttnArgs& a, int lo, int hi, int split) {
   const int from = lo & ~127;
   const int per = (max(hi - from, 1) + 128 * a.nsplit - 1) / (128 * a.nsplit) * 128;
@@ -326,6 +326,9 @@ RFX_DEV int count_tiles(const PagedAttnArgs& a, int bm, int lane) {
 // start of the argument segment) and the tile's number, so that this rare path
 // keeps nothing alive through the loops before it: what it needs held from there
 // cost 29 spilled scalar registers and 5 to 8 % with many rows over fp8 pages.
+// It is slow, a key at a time by one wave: 64 single tokens over 8,000 bf16 keys
+// of which one has a NaN 1.1 ms instead of 0.11, two prompts of 8,192 rows whose
+// last token has one 132 ms instead of 1.1.
 template <typename T, int ST, int DH>
 RFX_DEV void redo_row(int tile, int bm, int q, int64_t row, int head, int split, bool halves, float& M, float& L,
                       float* y) {
@@ -388,11 +391,12 @@ RFX_DEV void finish_row(const PagedAttnArgs& a, int tile, int bm, int q, int64_t
 // never rounded.  The waves' results meet in LDS at the end.
 //
 // 64 single tokens, 8 query heads of 256 on one K/V head: over 15,409 fp8 keys
-// at most (310 MB) 66-73 us, 4.2-4.7 TB/s; over 8,000 bf16 keys (525 MB) 104 us,
-// 5.0 TB/s, as a large copy.  One token over 817 keys 10 us, a chain of
-// latencies (lengths, table, K, V, the exchange).  fp32 is bound by its matrix
-// products at one wave to a SIMD: four prompts of 1,000 rows with 8 heads of 128
-// 356 us, 69 TFLOP/s of the 154 that a large fp32 product reaches.
+// at most (310 MB) 66 us, 4.7 TB/s; over 8,000 bf16 keys (525 MB) 102 us with the
+// merge, 5.1 TB/s, and fp32 keys (1.05 GB) 194 us, 5.4 TB/s, as a large copy.  One
+// token over 817 keys 9 us, a chain of latencies (lengths, table, K, V, the
+// exchange).  fp32 with many rows is bound by its matrix products at one wave to
+// a SIMD: four chunks of 1,000 rows over 2,000 keys, 8 heads of 128 on two K/V
+// heads, 342 us, 72 TFLOP/s of the 154 that a large fp32 product reaches.
 template <typename T, int ST, int DH>
 struct FewCfg {
   static constexpr bool Q8 = ST == REFLEX_STORE_FP8 || ST == REFLEX_STORE_INT8;
@@ -814,13 +818,13 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
 // barrier a tile.  The probabilities are rounded to bf16 once (two halves, as
 // with few rows, would double the second product).
 //
-// Two prompts of 8,192 rows with 32 heads of 128, causal: 1.13-1.17 ms, 940-970
-// TFLOP/s, matrix units busy for 53 % and vector issue for 56 % of the cycles
-// (the exponentials, maxima and roundings that cannot all hide).  One chunk of
-// 768 rows with 8 heads of 256 over 15,408 keys: 122 us, 790 TFLOP/s; the
-// products alone, by the single wave that a SIMD holds, take 96.  8-bit pages
-// cost a conversion of every fragment in every wave: prompts 1.37 (fp8) and
-// 1.71 ms (int8).
+// Two prompts of 8,192 rows with 32 heads of 128, causal: 1.09-1.13 ms, 975-1,010
+// TFLOP/s, matrix units busy for 54 % and vector issue for 56 % of the cycles:
+// the two overlap little, although two waves share a SIMD.  One chunk of 768 rows
+// with 8 heads of 256 over 15,408 keys: 121 us, 800 TFLOP/s, matrix units busy
+// for 42 % and vector issue for 31 %; without softmax, copies and LDS reads the
+// one wave of a SIMD took 96.  8-bit pages cost a conversion of every fragment
+// in every wave: prompts 1.31 (fp8) and 1.63 ms (int8).
 template <int ST, int DH>
 struct ManyCfg {
   static constexpr bool Q8 = ST == REFLEX_STORE_FP8 || ST == REFLEX_STORE_INT8;
@@ -863,7 +867,7 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
   // a CU may fill the chip exactly, and then the runs have to be of the tiles
   // that the batch has, not of the grid's: with those a chunk of 1,024 rows of 8
   // heads over 8,192 keys gave some XCDs one too many and took 159 us instead of
-  // 93.  (Narrower heads, two workgroups to a CU, lose 2 % to the counting.)
+  // 93 (now 88).  (Narrower heads, two workgroups to a CU, lose 2 % to the counting.)
   const int tiles = WIDE ? count_tiles(a, BM, lane) : grid_tiles;
   const int all = tiles * a.c.n_kv * a.nsplit, per = (all + 7) >> 3;
   const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
@@ -1336,10 +1340,10 @@ int64_t tile_bound(int64_t n_rows, int n_seqs, int group, int bm) {
 // Rows of a tile, by the rows of an average sequence (with one K/V head): 16 or
 // 32 with the few-row kernel, 128 with the many-row one.  fp32, which only the
 // first has, takes 32 where that makes two workgroups for every CU: seven
-// ragged chunks of up to 450 rows 23 us with 16 against 30, four of 4,000 rows
-// 430 against 360.  256-wide heads stay at 16, as queries and sums of 32 such
-// rows do not fit a wave's registers: four of 8,000 rows 755 us against 882,
-// over int8 pages 600 against 742.
+// ragged chunks of up to 450 rows 23 us with 16 against 31, four of 4,000 rows
+// 419 against 342.  256-wide heads stay at 16, as queries and sums of 32 such
+// rows do not fit a wave's registers: four of 8,000 rows 730 us against 736,
+// over int8 pages 594 against 705.
 int rows_of_tile(int64_t n_rows, int n_seqs, int group, int n_kv, int dh, int dtype) {
   const int64_t rows = n_rows * group / std::max<int64_t>(1, std::min<int64_t>(n_seqs, n_rows));
   if (rows <= 16) return 16;

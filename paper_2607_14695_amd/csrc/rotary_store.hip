@@ -121,9 +121,11 @@ template <typename T> RFX_DEV void sincos_for(double f, float* sn, float* cs) {
 // ---------------------------------------------------------------------------
 // rotary
 // ---------------------------------------------------------------------------
-// 24,576 rows of 8 heads of 256 in fp32 (403 MB read and written) take 86 us,
-// 4.7 TB/s, where a large copy reaches 4.9; 768 rows in bf16 5 us and eight rows
-// 4 us, the latency of positions, frequencies and rows.
+// 24,576 rows of 8 heads of 256 in fp32 (403 MB read and written) take 87 us,
+// 4.6 TB/s, where a large copy reaches 4.9-5.0; 768 rows in bf16 5 us and eight
+// rows 4 us, the latency of positions, frequencies and rows.  (Products in 64
+// bits too would leave only the result's rounding, 2.5e-8 of it instead of
+// 3.3e-8, and take 5 % longer.)
 template <typename T>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
   const int G = a.plan.head_dim >> 4;
@@ -269,10 +271,10 @@ template <> struct Raw8<bf16_t> {
 // blockIdx.z: 0 = K (rotated), 1 = V.  A wave takes 64 / G rows.  Bound by the
 // vector unit where keys are rotated for an 8-bit store: 32 frames of 768 keys
 // of 256 take 20 us with V, 8 us of them memory's.  Eight prompts with eight
-// heads of 128 (44,000 rows, 273 MB) 70 us, 3.9 TB/s: the angles' sines are taken
-// once for all heads.  (Measured slower: four times
-// the rows a wave, 22 us and, with eight 128-wide heads, 89 against 78 us; K and
-// V side by side in turn, 25 us.)
+// heads of 128 (44,000 rows) take 70 us into int8 pages (273 MB), 3.9 TB/s, and 76
+// into bf16 ones (360 MB), 4.8 TB/s: the angles' sines are taken once for all
+// heads.  (Measured slower: four times the rows a wave, 22 us and, with eight
+// 128-wide heads, 89 against 78 us; K and V side by side in turn, 25 us.)
 template <typename T, int ST>
 __global__ __launch_bounds__(256) void paged_write_kernel(const PagedWriteArgs a) {
   const int G = a.c.dh >> 4;  // 4, 8 or 16
@@ -393,7 +395,7 @@ RFX_DEV void decode8(const uint2& c, float scale, float* o) {
 
 // blockIdx.z: 0 = K, 1 = V; blockIdx.y: the head.  A wave takes U times 64 / G
 // rows, whose loads are all under way before the first is used.  The same prompts
-// 50 us, 5.4 TB/s.
+// 50 us from int8 pages, 5.4 TB/s; 69 from bf16 and 171 from fp32 ones, 5.2 and 4.2.
 template <typename T, int ST, int U>
 __global__ __launch_bounds__(256) void paged_read_kernel(const PagedReadArgs a) {
   constexpr bool Q = ST == REFLEX_STORE_FP8 || ST == REFLEX_STORE_INT8;
