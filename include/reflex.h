@@ -641,6 +641,101 @@ int reflex_paged_attention(const reflex_paged_cache* cache, const reflex_paged_b
                            const reflex_rows* out, int64_t n_rows, int32_t n_q_heads, int32_t dtype, float scale,
                            int32_t causal, int32_t window, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Drafted tokens.  A batch's rows may be a tree of drafted tokens instead of a
+ * run: each follows the cached tokens or an earlier row of its sequence, its
+ * parent.  Their K and V lie in the pages as any rows' do, row i of a sequence
+ * as token lengths[b] - n_b + i; what they see and where they stand is the
+ * tree's.
+ *
+ * mask: device uint64 [n_rows][mask_words], 1 to 64 words: bit j of row r's
+ * words (word j / 64, bit j % 64) says that row r sees row j of its own
+ * sequence.  Rows that it cannot name (from 64 * mask_words on) are seen by
+ * none.
+ *
+ * reflex_paged_tree fills it from the rows' parents: bit j of row i is set where
+ * j is i or one of its ancestors.  parents: device int32 [n_rows], indexes among
+ * the sequence's rows; what is not in [0, i) follows the cached tokens.
+ * positions (device int64 [n_rows], may be NULL): lengths[b] - n_b + the number
+ * of the row's ancestors, as reflex_paged_write takes them.  A row that the words
+ * cannot name sees no row and has the position of one without ancestors.  Rows of
+ * no sequence keep what is there.  The page table is not used.
+ * Errors: REFLEX_EINVAL, REFLEX_EHIP.
+ */
+int reflex_paged_tree(const reflex_paged_batch* batch, const int32_t* parents, int64_t n_rows, uint64_t* mask,
+                      int32_t mask_words, int64_t* positions, void* stream);
+
+/*
+ * Attention of drafted tokens: as reflex_paged_attention, in each respect and
+ * with its workspace, where row r sees the present tokens before its sequence's
+ * rows (j < lengths[b] - n_b) and those of the sequence's rows that its bits
+ * name.  A row may see nothing, itself included: then it gets zeros.
+ */
+int reflex_paged_tree_attention(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const reflex_rows* q,
+                                const reflex_rows* out, int64_t n_rows, int32_t n_q_heads, int32_t dtype, float scale,
+                                const uint64_t* mask, int32_t mask_words, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/*
+ * Go on from the accepted rows: for i < c_b, token lengths[b] - n_b + i takes K
+ * and V (codes and scales) of the sequence's row path[b][i], and lengths_out[b]
+ * becomes lengths[b] - n_b + c_b (at least 0).  path: device int32
+ * [n_seqs][max_path], strictly increasing up to c_b, as the rows of a way down a
+ * tree are; counts: device int32 [n_seqs], c_b = counts[b] cut to [0, min(n_b,
+ * max_path)].  A row outside [0, n_b), or whose token is absent, reads as zeros;
+ * what the places behind token c_b hold stays.  If path does not increase, what
+ * the accepted tokens hold is undefined.  Pages that rows move in belong to one
+ * sequence of the call.  lengths_out may be the batch's lengths; n_b is not cut
+ * to a number of rows here.
+ * Errors: REFLEX_EINVAL, REFLEX_EHIP.
+ */
+int reflex_paged_accept(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const int32_t* path,
+                        int32_t max_path, const int32_t* counts, int32_t* lengths_out, void* stream);
+
+/*
+ * Attention that also adds up what every key got: reflex_paged_attention, and
+ *   weights[slot of j][g] += sum over the batch's rows r that see token j, and
+ *                            over the query heads h of g, of softmax_j(...)
+ * weights: device fp32 [n_pages][n_kv_heads][page_size], added to where a row
+ * sees the token, and one key's sum at once, in fp32 and always in the same
+ * order.  A row with zeros as its result adds nothing; one whose scores make its
+ * result NaN adds NaN to all that it sees.  Pages whose weights are added to
+ * belong to one sequence of the call: where they are shared, additions may be
+ * lost.  A page that goes to another sequence needs its weights set to 0.
+ * Errors: as reflex_paged_attention, with a workspace of its own size.
+ */
+int reflex_paged_weighed_attention_workspace(const reflex_paged_cache* cache, const reflex_paged_batch* batch,
+                                             int64_t n_rows, int32_t n_q_heads, int32_t dtype, size_t* bytes);
+int reflex_paged_weighed_attention(const reflex_paged_cache* cache, const reflex_paged_batch* batch,
+                                   const reflex_rows* q, const reflex_rows* out, int64_t n_rows, int32_t n_q_heads,
+                                   int32_t dtype, float scale, int32_t causal, int32_t window, float* weights,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Cut every sequence that is longer than `keep` to that many tokens.  Each K/V
+ * head keeps its own: the first `sinks`, the last `recent`, and of those between
+ * the ones of greatest weight (weights as above; of equal ones the earlier
+ * tokens, -0 is 0, a NaN counts as -infinity, and absent tokens come last).  The
+ * kept tokens' K, V, scales and weights move to tokens 0 .. keep - 1 in their
+ * order, the weights of the places that are left become 0, and lengths_out[b] is
+ * min(lengths[b], keep).  Keys stay rotated by the positions that they were
+ * written with.  A length counts up to max_pages * page_size.
+ * kept (device int32 [n_seqs][n_kv_heads][keep], may be NULL): the tokens that
+ * were kept, increasing; of a sequence that was not cut its own, then -1.
+ * cu_rows is not read.  A kept token that is absent reads as zeros, with weight 0.
+ * Pages that tokens move in belong to one sequence of the call.  lengths_out may
+ * be the batch's lengths.
+ * keep: 1 to 2^30, at least sinks + recent; n_seqs * n_kv_heads <= 2^24.
+ * workspace: at least the bytes that reflex_paged_evict_workspace gives,
+ * 256-byte aligned; private to the call until its work is done.
+ * Errors: REFLEX_EINVAL, REFLEX_EHIP.
+ */
+int reflex_paged_evict_workspace(const reflex_paged_cache* cache, const reflex_paged_batch* batch, int32_t keep,
+                                 size_t* bytes);
+int reflex_paged_evict(const reflex_paged_cache* cache, const reflex_paged_batch* batch, float* weights, int32_t keep,
+                       int32_t sinks, int32_t recent, int32_t* kept, int32_t* lengths_out, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

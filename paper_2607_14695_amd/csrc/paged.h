@@ -104,6 +104,9 @@ struct PagedAttnArgs {
   int nsplit;        // key splits; with more than one, partials go to the workspace
   float* part_o;     // [n_rows * n_q][nsplit][dh]
   float2* part_ml;   // [n_rows * n_q][nsplit] (running maximum, sum)
+  const uint64_t* tree;  // kTree: [n_rows][tree_words], which of its sequence's rows a row sees
+  int tree_words;
+  float2* stats;     // kWeigh: [n_rows * n_q] (maximum, 1 / sum, or 0 for a row that sees nothing)
 };
 struct PagedAttnPlan {
   int nsplit;
@@ -112,5 +115,43 @@ struct PagedAttnPlan {
 PagedAttnPlan paged_attention_plan(const reflex_paged_cache& c, const reflex_paged_batch& b, int64_t n_rows, int n_q,
                                    int dtype, int window);
 template <typename T> hipError_t launch_paged_attention(const PagedAttnArgs& a, int store, hipStream_t s);
+template <typename T> hipError_t launch_paged_tree_attention(const PagedAttnArgs& a, int store, hipStream_t s);
+// keys: the length that the longest sequence is expected to have
+template <typename T>
+hipError_t launch_paged_weighed_attention(const PagedAttnArgs& a, int store, float* weights, int64_t keys, hipStream_t s);
+
+constexpr int kMaxTreeWords = 64, kMaxTreeRows = 64 * kMaxTreeWords;
+
+struct PagedTreeArgs {
+  Seqs q;
+  const int32_t* parents;
+  int64_t n_rows;
+  int words;
+  uint64_t* mask;  // [n_rows][words]
+  int64_t* pos;    // [n_rows], or null
+};
+hipError_t launch_paged_tree(const PagedTreeArgs& a, hipStream_t s);
+
+struct PagedAcceptArgs {
+  Pages c;
+  Seqs q;
+  const int32_t* path;    // [sequences][max_path]
+  const int32_t* counts;  // [sequences]
+  int max_path;
+  int32_t* lengths;       // written; may be q.len
+};
+hipError_t launch_paged_accept(const PagedAcceptArgs& a, int elem_bytes, int scaled, hipStream_t s);
+
+struct PagedEvictArgs {
+  Pages c;
+  Seqs q;
+  float* weights;      // [pages][heads][page size]
+  int keep, sinks, recent;
+  int32_t* kept;       // [sequences][heads][keep], or null
+  int32_t* lengths;    // written; may be q.len
+  int32_t* from;       // workspace: [sequences][heads][keep] page rows
+  int2* cut;           // workspace: [sequences][heads]
+};
+hipError_t launch_paged_evict(const PagedEvictArgs& a, int elem_bytes, int scaled, hipStream_t s);
 
 }  // namespace reflex

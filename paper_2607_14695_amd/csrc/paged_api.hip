@@ -88,6 +88,51 @@ Seqs seqs_of(const reflex_paged_batch* b) {
   return Seqs{b->cu_rows, b->lengths, b->page_table, b->n_seqs, b->max_pages};
 }
 
+int elem_bytes(const reflex_paged_cache* c) {
+  return c->store == REFLEX_STORE_F32 ? 4 : c->store == REFLEX_STORE_BF16 ? 2 : 1;
+}
+
+int check_words(int32_t words) { return words >= 1 && words <= kMaxTreeWords ? REFLEX_OK : REFLEX_EINVAL; }
+
+// The rows' maxima and sums lie behind the splits' partial results.
+size_t stats_at(size_t partials) { return (partials + 255) & ~(size_t)255; }
+
+int check_attention(const reflex_rows* q, const reflex_rows* out, int64_t n_rows, int32_t dtype, float scale,
+                    int32_t window, const void* workspace, size_t workspace_bytes, size_t need) {
+  RFX_CHECK(check_rows(q, n_rows, dtype));
+  RFX_CHECK(check_rows(out, n_rows, dtype));
+  const double s2 = fabs((double)scale) * 1.4426950408889634;
+  if (!(s2 <= (double)FLT_MAX) || window < 0) return REFLEX_EINVAL;
+  if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return REFLEX_EINVAL;
+  return REFLEX_OK;
+}
+
+void fill_attention(PagedAttnArgs& a, const reflex_paged_cache* cache, const reflex_paged_batch* batch,
+                    const reflex_rows* q, const reflex_rows* out, int64_t n_rows, int32_t n_q_heads, int32_t dtype,
+                    float scale, int32_t causal, int32_t window, void* workspace) {
+  const PagedAttnPlan p = paged_attention_plan(*cache, *batch, n_rows, n_q_heads, dtype, window);
+  a.c = pages_of(cache);
+  a.q = seqs_of(batch);
+  a.x = rows_of(q);
+  a.o = rows_of(out);
+  a.n_rows = n_rows;
+  a.n_q = n_q_heads;
+  a.group = n_q_heads / cache->n_kv_heads;
+  const double s2 = fabs((double)scale) * 1.4426950408889634, tiny = 0x1p-126;
+  // (scaled up by 2^64 and then cut off at 2^-126 a score of 2^128 is 2^-62: 0)
+  a.scale2 = (float)(s2 < tiny ? fmax(s2 * 0x1p64, tiny) : s2);
+  a.factor = (scale < 0.f ? -1.f : 1.f) * (s2 < tiny ? 0x1p-64f : 1.f);
+  a.causal = causal != 0;
+  a.window = window;
+  a.nsplit = p.nsplit;
+  const size_t rows = (size_t)n_rows * n_q_heads * p.nsplit;
+  a.part_o = reinterpret_cast<float*>(workspace);
+  a.part_ml = reinterpret_cast<float2*>(reinterpret_cast<char*>(workspace) + rows * cache->head_dim * sizeof(float));
+  a.tree = nullptr;
+  a.tree_words = 0;
+  a.stats = nullptr;
+}
+
 int done(hipError_t e) { return e == hipSuccess ? REFLEX_OK : hip_fail(e); }
 
 }  // namespace
@@ -217,34 +262,107 @@ int reflex_paged_attention(const reflex_paged_cache* cache, const reflex_paged_b
                            int32_t causal, int32_t window, void* workspace, size_t workspace_bytes, void* stream) {
   size_t need = 0;
   RFX_CHECK(reflex_paged_attention_workspace(cache, batch, n_rows, n_q_heads, dtype, &need));
-  RFX_CHECK(check_rows(q, n_rows, dtype));
-  RFX_CHECK(check_rows(out, n_rows, dtype));
-  const double s2 = fabs((double)scale) * 1.4426950408889634;
-  if (!(s2 <= (double)FLT_MAX) || window < 0) return REFLEX_EINVAL;
-  if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return REFLEX_EINVAL;
-  if (n_rows == 0 || batch->n_seqs == 0) return REFLEX_OK;
-  const PagedAttnPlan p = paged_attention_plan(*cache, *batch, n_rows, n_q_heads, dtype, window);
   PagedAttnArgs a;
-  a.c = pages_of(cache);
-  a.q = seqs_of(batch);
-  a.x = rows_of(q);
-  a.o = rows_of(out);
-  a.n_rows = n_rows;
-  a.n_q = n_q_heads;
-  a.group = n_q_heads / cache->n_kv_heads;
-  const double tiny = 0x1p-126;
-  // (scaled up by 2^64 and then cut off at 2^-126 a score of 2^128 is 2^-62: 0)
-  a.scale2 = (float)(s2 < tiny ? fmax(s2 * 0x1p64, tiny) : s2);
-  a.factor = (scale < 0.f ? -1.f : 1.f) * (s2 < tiny ? 0x1p-64f : 1.f);
-  a.causal = causal != 0;
-  a.window = window;
-  a.nsplit = p.nsplit;
-  const size_t rows = (size_t)n_rows * n_q_heads * p.nsplit;
-  a.part_o = reinterpret_cast<float*>(workspace);
-  a.part_ml = reinterpret_cast<float2*>(reinterpret_cast<char*>(workspace) + rows * cache->head_dim * sizeof(float));
+  RFX_CHECK(check_attention(q, out, n_rows, dtype, scale, window, workspace, workspace_bytes, need));
+  if (n_rows == 0 || batch->n_seqs == 0) return REFLEX_OK;
+  fill_attention(a, cache, batch, q, out, n_rows, n_q_heads, dtype, scale, causal, window, workspace);
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   return done(dtype == REFLEX_DTYPE_BF16 ? launch_paged_attention<bf16_t>(a, cache->store, s)
                                          : launch_paged_attention<float>(a, cache->store, s));
+}
+
+int reflex_paged_tree(const reflex_paged_batch* batch, const int32_t* parents, int64_t n_rows, uint64_t* mask,
+                      int32_t mask_words, int64_t* positions, void* stream) {
+  if (!batch || batch->n_seqs < 0 || n_rows < 0 || n_rows > kMaxRows) return REFLEX_EINVAL;
+  RFX_CHECK(check_words(mask_words));
+  if (n_rows == 0 || batch->n_seqs == 0) return REFLEX_OK;
+  if (!batch->cu_rows || !batch->lengths || !parents || !mask || ((uintptr_t)mask & 7) || ((uintptr_t)positions & 7))
+    return REFLEX_EINVAL;
+  const PagedTreeArgs a{seqs_of(batch), parents, n_rows, mask_words, mask, positions};
+  return done(launch_paged_tree(a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int reflex_paged_tree_attention(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const reflex_rows* q,
+                                const reflex_rows* out, int64_t n_rows, int32_t n_q_heads, int32_t dtype, float scale,
+                                const uint64_t* mask, int32_t mask_words, void* workspace, size_t workspace_bytes,
+                                void* stream) {
+  size_t need = 0;
+  RFX_CHECK(reflex_paged_attention_workspace(cache, batch, n_rows, n_q_heads, dtype, &need));
+  RFX_CHECK(check_words(mask_words));
+  PagedAttnArgs a;
+  RFX_CHECK(check_attention(q, out, n_rows, dtype, scale, 0, workspace, workspace_bytes, need));
+  if (n_rows == 0 || batch->n_seqs == 0) return REFLEX_OK;
+  if (!mask || ((uintptr_t)mask & 7)) return REFLEX_EINVAL;
+  fill_attention(a, cache, batch, q, out, n_rows, n_q_heads, dtype, scale, 0, 0, workspace);
+  a.tree = mask;
+  a.tree_words = mask_words;
+  const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  return done(dtype == REFLEX_DTYPE_BF16 ? launch_paged_tree_attention<bf16_t>(a, cache->store, s)
+                                         : launch_paged_tree_attention<float>(a, cache->store, s));
+}
+
+int reflex_paged_accept(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const int32_t* path,
+                        int32_t max_path, const int32_t* counts, int32_t* lengths, void* stream) {
+  RFX_CHECK(check_cache(cache));
+  RFX_CHECK(check_batch(batch, cache, 1));
+  if (max_path < 0) return REFLEX_EINVAL;
+  if (batch->n_seqs == 0) return REFLEX_OK;
+  if ((max_path > 0 && !path) || !counts || !lengths) return REFLEX_EINVAL;
+  const PagedAcceptArgs a{pages_of(cache), seqs_of(batch), path, counts, max_path, lengths};
+  return done(launch_paged_accept(a, elem_bytes(cache), cache->store >= REFLEX_STORE_FP8, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int reflex_paged_weighed_attention_workspace(const reflex_paged_cache* cache, const reflex_paged_batch* batch,
+                                             int64_t n_rows, int32_t n_q_heads, int32_t dtype, size_t* bytes) {
+  RFX_CHECK(reflex_paged_attention_workspace(cache, batch, n_rows, n_q_heads, dtype, bytes));
+  if (n_rows > 0 && batch->n_seqs > 0) *bytes = stats_at(*bytes) + (size_t)n_rows * n_q_heads * sizeof(float2);
+  return REFLEX_OK;
+}
+
+int reflex_paged_weighed_attention(const reflex_paged_cache* cache, const reflex_paged_batch* batch,
+                                   const reflex_rows* q, const reflex_rows* out, int64_t n_rows, int32_t n_q_heads,
+                                   int32_t dtype, float scale, int32_t causal, int32_t window, float* weights,
+                                   void* workspace, size_t workspace_bytes, void* stream) {
+  size_t need = 0, part = 0;
+  RFX_CHECK(reflex_paged_weighed_attention_workspace(cache, batch, n_rows, n_q_heads, dtype, &need));
+  RFX_CHECK(reflex_paged_attention_workspace(cache, batch, n_rows, n_q_heads, dtype, &part));
+  PagedAttnArgs a;
+  RFX_CHECK(check_attention(q, out, n_rows, dtype, scale, window, workspace, workspace_bytes, need));
+  if (n_rows == 0 || batch->n_seqs == 0) return REFLEX_OK;
+  if (!weights || ((uintptr_t)weights & 3)) return REFLEX_EINVAL;
+  fill_attention(a, cache, batch, q, out, n_rows, n_q_heads, dtype, scale, causal, window, workspace);
+  a.stats = reinterpret_cast<float2*>(reinterpret_cast<char*>(workspace) + stats_at(part));
+  const int64_t cap = (int64_t)batch->max_pages * cache->page_size;
+  const int64_t keys = batch->max_length > 0 && batch->max_length < cap ? batch->max_length : cap;
+  const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  return done(dtype == REFLEX_DTYPE_BF16 ? launch_paged_weighed_attention<bf16_t>(a, cache->store, weights, keys, s)
+                                         : launch_paged_weighed_attention<float>(a, cache->store, weights, keys, s));
+}
+
+int reflex_paged_evict_workspace(const reflex_paged_cache* cache, const reflex_paged_batch* batch, int32_t keep,
+                                 size_t* bytes) {
+  if (!bytes) return REFLEX_EINVAL;
+  RFX_CHECK(check_cache(cache));
+  RFX_CHECK(check_batch(batch, cache, 1));
+  if (keep < 1 || keep > (1 << 30) || (int64_t)batch->n_seqs * cache->n_kv_heads > (1 << 24)) return REFLEX_EINVAL;
+  *bytes = (size_t)batch->n_seqs * cache->n_kv_heads * (sizeof(int2) + (size_t)keep * sizeof(int32_t));
+  return REFLEX_OK;
+}
+
+int reflex_paged_evict(const reflex_paged_cache* cache, const reflex_paged_batch* batch, float* weights, int32_t keep,
+                       int32_t sinks, int32_t recent, int32_t* kept, int32_t* lengths, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  RFX_CHECK(reflex_paged_evict_workspace(cache, batch, keep, &need));
+  if (sinks < 0 || recent < 0 || (int64_t)sinks + recent > keep) return REFLEX_EINVAL;
+  if (batch->n_seqs == 0) return REFLEX_OK;
+  if (!weights || ((uintptr_t)weights & 3) || !lengths) return REFLEX_EINVAL;
+  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return REFLEX_EINVAL;
+  int2* const cut = reinterpret_cast<int2*>(workspace);
+  const PagedEvictArgs a{pages_of(cache), seqs_of(batch), weights, keep,    sinks, recent,
+                         kept,            lengths,        reinterpret_cast<int32_t*>(cut + batch->n_seqs * cache->n_kv_heads),
+                         cut};
+  return done(launch_paged_evict(a, elem_bytes(cache), cache->store >= REFLEX_STORE_FP8, reinterpret_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

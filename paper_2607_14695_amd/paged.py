@@ -20,6 +20,7 @@ from .reflex import (DTYPE_BF16, DTYPE_F32, STORE_BF16, STORE_F32, STORE_FP8, ST
 _DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
 _STORES = {torch.float32: STORE_F32, torch.bfloat16: STORE_BF16, torch.float8_e4m3fn: STORE_FP8,
            torch.int8: STORE_INT8}
+MAX_TREE_WORDS = 64
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
 
@@ -151,6 +152,35 @@ class PagedBatch:
                              n, page_table.shape[1], max_length, 0)
         self._ref = ctypes.byref(self.c)
 
+    def tree(self, parents: torch.Tensor, max_rows: int = 0,
+             out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """(mask, positions) of drafted tokens: ``parents`` (int32 [rows]) names each row's parent among its
+        sequence's rows, -1 for one that follows the cached tokens.  ``mask`` int64 [rows, words]: as bits the rows
+        that each row sees, itself and its ancestors, for ``PagedCache.attend_tree``; ``positions`` int64 [rows] for
+        ``PagedCache.write`` and ``Rotary.apply``.  ``max_rows``: the most rows of a sequence (0: all rows), at most
+        4,096.  Without ``out``, rows of no sequence are undefined."""
+        n = parents.shape[0] if parents.dim() == 1 else -1
+        p = _index(parents, (n,), torch.int32, "parents", self.device)
+        if out is None:
+            words = -(-(max_rows if max_rows > 0 else max(n, 1)) // 64)
+            if not 1 <= words <= MAX_TREE_WORDS:
+                raise ValueError(f"a tree has at most {64 * MAX_TREE_WORDS} rows a sequence, not {max_rows or n}")
+            out = (torch.empty((n, words), dtype=torch.int64, device=self.device),
+                   torch.empty(n, dtype=torch.int64, device=self.device))
+        mask, positions = out
+        m, words = _mask(mask, n, self.device)
+        pos = _index(positions, (n,), torch.int64, "positions", self.device)
+        _call(self.device, "reflex_paged_tree", load_library().reflex_paged_tree, self._ref, p, n, m, words, pos)
+        return mask, positions
+
+
+def _mask(mask: torch.Tensor, n: int, device: torch.device) -> Tuple[int, int]:
+    """(pointer, words of a row) of a tree's bits."""
+    words = mask.shape[1] if mask.dim() == 2 else 0
+    if not 1 <= words <= MAX_TREE_WORDS:
+        raise ValueError(f"mask is [rows, 1 to {MAX_TREE_WORDS} words], got {tuple(mask.shape)}")
+    return _index(mask, (n, words), torch.int64, "mask", device), words
+
 
 class PagedCache:
     """A paged K/V cache over the caller's tensors: k, v [pages, kv heads, page size, head dim] in float32, bfloat16,
@@ -229,16 +259,37 @@ class PagedCache:
         return out
 
     def attend(self, batch: PagedBatch, q: torch.Tensor, causal: bool = True, window: int = 0,
-               scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+               scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+               weights: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of the batch's rows q [rows, heads, head dim] over the pages of their sequences, which hold
         the rows' own keys and values.  Scores are scaled by ``scale`` (default head_dim ** -0.5).  Without
         ``out``, rows of no sequence are undefined.  The workspace comes from torch's allocator, on the current
-        stream."""
+        stream.
+        ``weights`` (float32 [pages, kv heads, page size], see ``zero_weights``): every key's probabilities, summed
+        over the rows and the query heads of its K/V head, are added to it; pages that sequences share are not
+        weighed."""
+        _int32(window, "window")
+        if weights is None:
+            return self._attend(batch, q, scale, out, "reflex_paged_attention", "reflex_paged_attention_workspace",
+                                int(causal), window)
+        return self._attend(batch, q, scale, out, "reflex_paged_weighed_attention",
+                            "reflex_paged_weighed_attention_workspace", int(causal), window, self._weights(weights))
+
+    def attend_tree(self, batch: PagedBatch, q: torch.Tensor, mask: torch.Tensor, scale: Optional[float] = None,
+                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of drafted tokens q [rows, heads, head dim], whose keys and values are in the pages: over the
+        tokens before their sequence's rows, and those of these rows that ``mask`` (int64 [rows, words], see
+        ``PagedBatch.tree``) names.  Else as ``attend``."""
+        m, words = _mask(mask, q.shape[0] if q.dim() else 0, self.device)
+        return self._attend(batch, q, scale, out, "reflex_paged_tree_attention", "reflex_paged_attention_workspace",
+                            m, words)
+
+    def _attend(self, batch: PagedBatch, q: torch.Tensor, scale: Optional[float], out: Optional[torch.Tensor],
+                call: str, space: str, *args) -> torch.Tensor:
         if q.dim() != 3:
             raise ValueError(f"q is [rows, heads, head_dim], got {tuple(q.shape)}")
         n, heads, dh = q.shape
         dt = _dtype(q.dtype)
-        _int32(window, "window")
         qr = _rows(q, n, heads, self.head_dim, self.device, "q")
         if out is None:
             out = torch.empty((n, heads, dh), dtype=q.dtype, device=self.device)
@@ -249,12 +300,54 @@ class PagedCache:
             yr = _rows(out, n, heads, dh, self.device, "out")
         ref = self._batch(batch)
         need = ctypes.c_size_t(0)
-        status = self.lib.reflex_paged_attention_workspace(self._ref, ref, n, heads, dt, ctypes.byref(need))
+        status = getattr(self.lib, space)(self._ref, ref, n, heads, dt, ctypes.byref(need))
         if status:
-            _check(status, "reflex_paged_attention_workspace")
+            _check(status, space)
         nb = need.value
         ws = torch.empty(nb, dtype=torch.uint8, device=self.device) if nb else None
-        _call(self.device, "reflex_paged_attention", self.lib.reflex_paged_attention, self._ref, ref,
-              ctypes.byref(qr), ctypes.byref(yr), n, heads, dt, self.head_dim ** -0.5 if scale is None else scale,
-              int(causal), window, ws.data_ptr() if nb else None, nb)
+        _call(self.device, call, getattr(self.lib, call), self._ref, ref, ctypes.byref(qr), ctypes.byref(yr), n, heads,
+              dt, self.head_dim ** -0.5 if scale is None else scale, *args, ws.data_ptr() if nb else None, nb)
         return out
+
+    def accept(self, batch: PagedBatch, path: torch.Tensor, counts: torch.Tensor) -> None:
+        """Go on from accepted drafted tokens: rows path[b][:counts[b]] of sequence b's rows (int32 [sequences, most]
+        and [sequences], increasing) become the tokens behind the cached ones, and the batch's lengths end with
+        them, written where the batch's tensor holds them."""
+        n = batch.c.n_seqs
+        most = path.shape[1] if path.dim() == 2 else -1
+        p = _index(path, (n, most), torch.int32, "path", self.device)
+        c = _index(counts, (n,), torch.int32, "counts", self.device)
+        _call(self.device, "reflex_paged_accept", self.lib.reflex_paged_accept, self._ref, self._batch(batch),
+              p if most else None, most, c, batch.c.lengths)
+
+    def zero_weights(self) -> torch.Tensor:
+        """A tensor for the weights of every key of the cache, of zeros."""
+        return torch.zeros(self.k.shape[:3], dtype=torch.float32, device=self.device)
+
+    def _weights(self, weights: torch.Tensor) -> int:
+        if weights.requires_grad or _dual_level():
+            _no_gradient(weights, "weights")
+        return _index(weights, self.k.shape[:3], torch.float32, "weights", self.device)
+
+    def evict(self, batch: PagedBatch, weights: torch.Tensor, keep: int, sinks: int = 0, recent: int = 0,
+              kept: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Cut every sequence that is longer than ``keep`` to that many tokens: for each K/V head its first
+        ``sinks``, its last ``recent`` and the others of greatest weight, moved together in order with their
+        weights; the weights of the places that are left become 0, and the batch's lengths are written where its
+        tensor holds them.  Returns ``kept`` (int32 [sequences, kv heads, keep]): the tokens that were kept, with -1
+        behind those of a shorter sequence.  Pages of the call's sequences are not shared."""
+        for x, what in ((keep, "keep"), (sinks, "sinks"), (recent, "recent")):
+            _int32(x, what)
+        ref, w = self._batch(batch), self._weights(weights)
+        need = ctypes.c_size_t(0)
+        status = self.lib.reflex_paged_evict_workspace(self._ref, ref, keep, ctypes.byref(need))
+        if status:
+            _check(status, "reflex_paged_evict_workspace")
+        shape = (batch.c.n_seqs, self.n_kv_heads, keep)
+        if kept is None:
+            kept = torch.empty(shape, dtype=torch.int32, device=self.device)
+        at = _index(kept, shape, torch.int32, "kept", self.device)
+        ws = torch.empty(need.value, dtype=torch.uint8, device=self.device)
+        _call(self.device, "reflex_paged_evict", self.lib.reflex_paged_evict, self._ref, ref, w, keep, sinks, recent, at,
+              batch.c.lengths, ws.data_ptr(), need.value)
+        return kept
