@@ -399,7 +399,9 @@ def _handles(s):
     case = s["case"]
     if case["op"] != "tree":
         s["cache"] = PagedCache(s["k"], s["v"], s.get("k_scale"), s.get("v_scale"))
-    s["batch"] = PagedBatch(s["cu"], s["lengths"], s["table"], max_length=max(_lengths(case)[1]))
+    new, length = _lengths(case)
+    s["batch"] = PagedBatch(s["cu"], s["lengths"], s["table"], max_length=max(length))
+    s["most"] = max(new)
 
 
 def run(state):
@@ -412,7 +414,7 @@ def run(state):
         if "batch" not in s:
             _handles(s)
         if op == "tree":
-            return list(s["batch"].tree(s["parents"], max_rows=max(_lengths(s["case"])[0])))
+            return list(s["batch"].tree(s["parents"], max_rows=s["most"]))
         if op == "verify":
             return s["cache"].attend_tree(s["batch"], s["q"], s["mask"])
         if op == "weigh":
