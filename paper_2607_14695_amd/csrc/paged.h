@@ -107,6 +107,10 @@ struct PagedAttnArgs {
   const uint64_t* tree;  // kTree: [n_rows][tree_words], which of its sequence's rows a row sees
   int tree_words;
   float2* stats;     // kWeigh: [n_rows * n_q] (maximum, 1 / sum, or 0 for a row that sees nothing)
+  float* scores;     // kWeigh: [n_rows * n_q][score_pitch] in units of log2 e, if row_splits is 0; else the
+                     // row splits' sums [row_splits][sequences * K/V heads][score_pitch]
+  int64_t score_pitch;
+  int row_splits;
 };
 struct PagedAttnPlan {
   int nsplit;
@@ -114,6 +118,14 @@ struct PagedAttnPlan {
 };
 PagedAttnPlan paged_attention_plan(const reflex_paged_cache& c, const reflex_paged_batch& b, int64_t n_rows, int n_q,
                                    int dtype, int window);
+// How weighed attention comes to the keys' sums: from kept scores (row_splits
+// 0), or from scores that are formed again by so many workgroups for the same keys.
+struct PagedWeighPlan {
+  int row_splits;
+  int64_t pitch;  // keys that the table holds, or 0
+  size_t bytes;   // of the scores or of the splits' sums
+};
+PagedWeighPlan paged_weigh_plan(const reflex_paged_cache& c, const reflex_paged_batch& b, int64_t n_rows, int n_q, int dtype);
 template <typename T> hipError_t launch_paged_attention(const PagedAttnArgs& a, int store, hipStream_t s);
 template <typename T> hipError_t launch_paged_tree_attention(const PagedAttnArgs& a, int store, hipStream_t s);
 // keys: the length that the longest sequence is expected to have
@@ -152,6 +164,6 @@ struct PagedEvictArgs {
   int32_t* from;       // workspace: [sequences][heads][keep] page rows
   int2* cut;           // workspace: [sequences][heads]
 };
-hipError_t launch_paged_evict(const PagedEvictArgs& a, int elem_bytes, int scaled, hipStream_t s);
+hipError_t launch_paged_evict(const PagedEvictArgs& a, int elem_bytes, int scaled, int64_t keys, hipStream_t s);
 
 }  // namespace reflex

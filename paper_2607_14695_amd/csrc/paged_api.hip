@@ -92,10 +92,17 @@ int elem_bytes(const reflex_paged_cache* c) {
   return c->store == REFLEX_STORE_F32 ? 4 : c->store == REFLEX_STORE_BF16 ? 2 : 1;
 }
 
+// the length that the longest sequence is expected to have
+int64_t expected_keys(const reflex_paged_cache* c, const reflex_paged_batch* b) {
+  const int64_t cap = (int64_t)b->max_pages * c->page_size;
+  return b->max_length > 0 && b->max_length < cap ? b->max_length : cap;
+}
+
 int check_words(int32_t words) { return words >= 1 && words <= kMaxTreeWords ? REFLEX_OK : REFLEX_EINVAL; }
 
-// The rows' maxima and sums lie behind the splits' partial results.
-size_t stats_at(size_t partials) { return (partials + 255) & ~(size_t)255; }
+// In weighed attention the rows' maxima and sums lie behind the splits' partial
+// results, and the scores behind these.
+size_t whole_256(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
 int check_attention(const reflex_rows* q, const reflex_rows* out, int64_t n_rows, int32_t dtype, float scale,
                     int32_t window, const void* workspace, size_t workspace_bytes, size_t need) {
@@ -131,6 +138,9 @@ void fill_attention(PagedAttnArgs& a, const reflex_paged_cache* cache, const ref
   a.tree = nullptr;
   a.tree_words = 0;
   a.stats = nullptr;
+  a.scores = nullptr;
+  a.score_pitch = 0;
+  a.row_splits = 1;
 }
 
 int done(hipError_t e) { return e == hipSuccess ? REFLEX_OK : hip_fail(e); }
@@ -315,7 +325,11 @@ int reflex_paged_accept(const reflex_paged_cache* cache, const reflex_paged_batc
 int reflex_paged_weighed_attention_workspace(const reflex_paged_cache* cache, const reflex_paged_batch* batch,
                                              int64_t n_rows, int32_t n_q_heads, int32_t dtype, size_t* bytes) {
   RFX_CHECK(reflex_paged_attention_workspace(cache, batch, n_rows, n_q_heads, dtype, bytes));
-  if (n_rows > 0 && batch->n_seqs > 0) *bytes = stats_at(*bytes) + (size_t)n_rows * n_q_heads * sizeof(float2);
+  if (n_rows > 0 && batch->n_seqs > 0) {
+    const size_t rows = (size_t)n_rows * n_q_heads;
+    *bytes = whole_256(whole_256(*bytes) + rows * sizeof(float2)) +
+             paged_weigh_plan(*cache, *batch, n_rows, n_q_heads, dtype).bytes;
+  }
   return REFLEX_OK;
 }
 
@@ -331,9 +345,13 @@ int reflex_paged_weighed_attention(const reflex_paged_cache* cache, const reflex
   if (n_rows == 0 || batch->n_seqs == 0) return REFLEX_OK;
   if (!weights || ((uintptr_t)weights & 3)) return REFLEX_EINVAL;
   fill_attention(a, cache, batch, q, out, n_rows, n_q_heads, dtype, scale, causal, window, workspace);
-  a.stats = reinterpret_cast<float2*>(reinterpret_cast<char*>(workspace) + stats_at(part));
-  const int64_t cap = (int64_t)batch->max_pages * cache->page_size;
-  const int64_t keys = batch->max_length > 0 && batch->max_length < cap ? batch->max_length : cap;
+  char* const stats = reinterpret_cast<char*>(workspace) + whole_256(part);
+  a.stats = reinterpret_cast<float2*>(stats);
+  const PagedWeighPlan p = paged_weigh_plan(*cache, *batch, n_rows, n_q_heads, dtype);
+  a.row_splits = p.row_splits;
+  a.score_pitch = p.pitch;
+  if (p.bytes) a.scores = reinterpret_cast<float*>(stats + whole_256((size_t)n_rows * n_q_heads * sizeof(float2)));
+  const int64_t keys = expected_keys(cache, batch);
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   return done(dtype == REFLEX_DTYPE_BF16 ? launch_paged_weighed_attention<bf16_t>(a, cache->store, weights, keys, s)
                                          : launch_paged_weighed_attention<float>(a, cache->store, weights, keys, s));
@@ -362,7 +380,8 @@ int reflex_paged_evict(const reflex_paged_cache* cache, const reflex_paged_batch
   const PagedEvictArgs a{pages_of(cache), seqs_of(batch), weights, keep,    sinks, recent,
                          kept,            lengths,        reinterpret_cast<int32_t*>(cut + batch->n_seqs * cache->n_kv_heads),
                          cut};
-  return done(launch_paged_evict(a, elem_bytes(cache), cache->store >= REFLEX_STORE_FP8, reinterpret_cast<hipStream_t>(stream)));
+  return done(launch_paged_evict(a, elem_bytes(cache), cache->store >= REFLEX_STORE_FP8, expected_keys(cache, batch),
+                                 reinterpret_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

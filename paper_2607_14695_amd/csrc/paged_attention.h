@@ -11,7 +11,7 @@
 // MODE says what a row sees and what is kept beside its result: kPlain a run of
 // keys, kTree the cached tokens and those of the call's rows whose bits are set,
 // kWeigh a run of keys, with every row's maximum and sum written for the sums of
-// its probabilities.  Each mode is compiled in a file of its own.
+// its probabilities, kKept (few rows) its scores too.  Each mode is compiled in a file of its own.
 #pragma once
 
 #include <algorithm>
@@ -23,7 +23,7 @@ namespace reflex {
 
 namespace {
 
-constexpr int kPlain = 0, kTree = 1, kWeigh = 2;
+constexpr int kPlain = 0, kTree = 1, kWeigh = 2, kKept = 3;
 
 // Running maxima start here instead of at -infinity, so that a row that sees
 // nothing has exp2(-infinity - m) = 0 and not NaN.
@@ -199,6 +199,13 @@ template <int N, typename F> RFX_DEV void static_for(F&& f) {
 
 // all but this wave's newest N copies have landed
 template <int N> RFX_DEV void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+// A store of 16 bytes per lane that the counts of wait_copies may include: all
+// lanes' and one instruction, at its place.  (Stores are counted with the loads,
+// in order.  The last of the four wait states before its data may be written
+// again is taken here.)
+RFX_DEV void store_counted(float* p, const f32x4_v& v) {
+  asm volatile("global_store_dwordx4 %0, %1, off\n\ts_nop 3" :: "v"(p), "v"(v) : "memory");
+}
 // LDS reads issued so far have their values: what they read may be overwritten
 RFX_DEV void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
@@ -394,7 +401,7 @@ RFX_DEV void finish_row(const PagedAttnArgs& a, int tile, int bm, int q, int64_t
   const int lane = threadIdx.x & 63;
   if (a.nsplit == 1) {
     store_row<T, DH>(a, row, head, L, y);
-    if constexpr (MODE == kWeigh)
+    if constexpr (MODE == kWeigh || MODE == kKept)
       if (lane == 0) a.stats[row * a.n_q + head] = make_float2(M, L == 0.f ? 0.f : 1.f / L);
     return;
   }
@@ -502,6 +509,22 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
       qf[m][k] = r < t.rows ? ld16(qp + d) : zero16();
     }
     scale_frags(qf[m], a.factor, T(0));
+    // (the compiler's own wait for the queries has to lie here: in the loop it would
+    // be one for the copies and the counted stores too)
+    if constexpr (MODE != kPlain) {
+#pragma unroll
+      for (int k = 0; k < NKS; ++k)
+        asm volatile("" : "+v"(qf[m][k].x), "+v"(qf[m][k].y), "+v"(qf[m][k].z), "+v"(qf[m][k].w));
+    }
+  }
+  float* score_row[MR];  // kKept: where a row's scores go; those of no row go behind the others, where none reads them
+#pragma unroll
+  for (int m = 0; m < MR; ++m) {
+    if constexpr (MODE == kKept) {
+      const int r = t.r0 + 16 * m + c16, tok = r / a.group;
+      const int64_t id = r < t.rows ? (t.first_row + tok) * a.n_q + kvh * a.group + (r - tok * a.group) : a.n_rows * a.n_q;
+      score_row[m] = a.scores + id * a.score_pitch;
+    }
   }
   f32x4_v o[MR][NDB];
   float mx[MR], sum[MR];
@@ -579,6 +602,9 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
     };
     constexpr uint64_t kAll = KT == 64 ? ~0ull : (1ull << KT) - 1;
     constexpr int NC = NI + (Q8 ? 1 : 0);
+    // stores of a tile's scores, between the next K copies and the next V copies
+    constexpr int NST = MODE == kKept ? MR * NKB : 0;
+    static_assert(NC + NST < 64, "the counter's range");
 
     int r_cur = row_of(wave);
     if (wave < n_t) {
@@ -592,7 +618,8 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
       const bool easy = in_page && __ballot(r_next >= 0) == kAll;
       const int key0 = seg + x * KT;
       const uint64_t present = __ballot(r_cur >= 0);
-      wait_copies<NC>();
+      if (NST > 0 && x != wave) wait_copies<NC + NST>();
+      else wait_copies<NC>();
       // S^T: block kb holds keys 16 kb + 4 g + i of query row c16
       f32x4_v s[MR][NKB];
 #pragma unroll
@@ -694,6 +721,7 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
             s[m][b][i] = v;
             top = fmaxf(top, v);
           }
+          if constexpr (MODE == kKept) store_counted(score_row[m] + key0 + 16 * b + 4 * g, s[m][b]);
         }
         top = across_rows(top, max2);
         if (__ballot(top > mx[m] + kSlack)) {
@@ -716,8 +744,8 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
         sum[m] += add;
       }
 
-      if (more) wait_copies<NC>();  // (the last tile has nothing newer under way)
-      else wait_copies<0>();
+      if (more) wait_copies<NC + NST>();  // (the last tile has no newer copies under way)
+      else wait_copies<NST>();
       if (Q8) {
 #pragma unroll
         for (int b = 0; b < NKB; ++b) {
@@ -1380,7 +1408,7 @@ __global__ __launch_bounds__(256) void paged_attn_merge_kernel(const PagedAttnAr
     }
   }
   store_row<T, DH>(a, row, (int)(id - row * a.n_q), L, y);
-  if constexpr (MODE == kWeigh)
+  if constexpr (MODE == kWeigh || MODE == kKept)
     if (lane == 0) a.stats[id] = make_float2(M, L == 0.f ? 0.f : 1.f / L);
 }
 
@@ -1409,7 +1437,7 @@ hipError_t launch_shape(const PagedAttnArgs& a, hipStream_t s) {
                               sizeof(T) == 2 ? REFLEX_DTYPE_BF16 : REFLEX_DTYPE_F32);
   const int64_t tiles = tile_bound(a.n_rows, a.q.n, a.group, bm);
   const dim3 grid((unsigned)tiles, (unsigned)(a.c.n_kv * a.nsplit));
-  if constexpr (sizeof(T) == 2) {
+  if constexpr (sizeof(T) == 2 && MODE != kKept) {
     if (bm == 128) {
       const unsigned n = (unsigned)((tiles * a.c.n_kv * a.nsplit + 7) / 8 * 8);
       RFX_LAUNCH((paged_attn_many_kernel<MODE, ST, DH>), dim3(n), dim3(256), 0, s, a, (int)tiles);

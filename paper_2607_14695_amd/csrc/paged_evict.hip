@@ -3,6 +3,8 @@
 //
 // Two kernels.  The first chooses (one workgroup to a sequence and K/V head);
 // the second moves rows, scales and weights and writes the lengths.
+#include <algorithm>
+
 #include "paged.h"
 
 namespace reflex {
@@ -17,21 +19,37 @@ RFX_DEV uint32_t order_of(float w) {
   return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
 }
 
-constexpr int kHeld = 32768;  // keys held in LDS; those of a longer sequence are read again
 constexpr int kBins = 2048;
+constexpr int kCopies = 4;        // of the histogram: a lane adds to copy lane % 4, which divides the conflicts of
+constexpr int kPitch = kBins + 16;  // equal digits; the copies' equal bins lie in different banks
+constexpr int kTable = 4096;      // table entries held in LDS, if that is all of them
+
+// Sum of a value over the lanes up to this one: within 16 lanes, then across them.
+RFX_DEV int lanes_up_to(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15, 31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
 
 // The least of the `need` greatest keys is found digit by digit (11, 11 and 10
 // bits): a histogram of the digits of those keys that agree so far, summed from
 // the top.  Counts are whole numbers, so the order of the additions does not
-// matter.  Then every wave counts the greater and the equal keys of a run of
-// tokens, and writes the chosen ones behind those of the waves before it.
+// matter.  Then every wave counts the greater and the equal keys of its tokens,
+// and writes the chosen ones behind those of the waves before it.
+//
+// A wave has a run of tokens, 64 at a time, the first HELD of these in registers
+// (longer sequences than the launch expected read the others again).
+template <int HELD>
 __global__ __launch_bounds__(1024) void paged_choose_kernel(const PagedEvictArgs a) {
-  __shared__ uint32_t held[kHeld];
-  __shared__ uint32_t hist[kBins];
-  __shared__ uint32_t part[16];
+  __shared__ uint32_t hist[kCopies * kPitch];
+  __shared__ int32_t table[kTable];
+  __shared__ __attribute__((aligned(16))) int part[16], part_eq[16];
   __shared__ int found, above;
-  __shared__ int2 waves[16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t list = blockIdx.x;
   const int b = (int)(list / a.c.n_kv), g = (int)(list - (int64_t)b * a.c.n_kv);
   const int raw = a.q.len[b];
@@ -47,49 +65,86 @@ __global__ __launch_bounds__(1024) void paged_choose_kernel(const PagedEvictArgs
   }
   const int lo = a.sinks, hi = len - a.recent, n = hi - lo;
   const int need = a.keep - a.sinks - a.recent;
-  const int64_t hoff = (int64_t)g << a.c.shift;
+  const int shift = a.c.shift, n_kv = a.c.n_kv, n_pages = a.c.n_pages;
+  const int hoff = g << shift;
+  const int entries = ((len - 1) >> shift) + 1;
+  const bool in_lds = entries <= kTable;
+  const int32_t* const mine = a.q.table + (int64_t)b * a.q.max_pages;
+  if (in_lds)
+    for (int e = tid; e < entries; e += 1024) table[e] = mine[e];
+  for (int i = tid; i < kCopies * kPitch; i += 1024) hist[i] = 0;
+  __syncthreads();
+  // page row of token j < len, or -1
   auto row_of = [&](int j) __attribute__((always_inline)) {
-    const int r = page_row(a.c, a.q, b, j);
-    return r < 0 ? -1 : r + (int)hoff;
+    const int page = in_lds ? table[j >> shift] : mine[j >> shift];
+    return (unsigned)page < (unsigned)n_pages ? ((page * n_kv) << shift) + (j & ((1 << shift) - 1)) + hoff : -1;
   };
-  auto read = [&](int j) __attribute__((always_inline)) {
-    const int r = row_of(lo + j);
-    return r < 0 ? 0u : order_of(a.weights[r]);
-  };
-  for (int j = tid; j < min(n, kHeld); j += 1024) held[j] = read(j);
-  auto key_of = [&](int j) __attribute__((always_inline)) { return j < kHeld ? held[j] : read(j); };
-
-  uint32_t top = 0;   // the digits found so far
-  int left = need;    // of the keys that have them, how many are chosen
-  for (int pass = 0; pass < 3 && need > 0; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
-    for (int i = tid; i < kBins; i += 1024) hist[i] = 0;
-    __syncthreads();
-    for (int j = tid; j < n; j += 1024) {
-      const uint32_t k = key_of(j);
-      if (pass == 0 || k >> (pass == 1 ? 21 : 10) == top) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
-    }
-    __syncthreads();
-    // thread t has bins 2 t', 2 t' + 1 with t' counted from the top
-    const int t = 1023 - tid;
-    const uint32_t h1 = hist[2 * t + 1], h0 = hist[2 * t];
-    uint32_t sum = h0 + h1;
+  const int chunks = (n + 1023) / 1024, first = wave * chunks * 64 + lane;
+  uint32_t key[HELD];
+  {
+    int r[HELD];
+    float w[HELD];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t v = __shfl_up(sum, o, 64);
-      if (lane >= o) sum += v;
+    for (int t = 0; t < HELD; ++t) r[t] = t < chunks ? row_of(lo + min(first + 64 * t, n - 1)) : -1;
+#pragma unroll
+    for (int t = 0; t < HELD; ++t) w[t] = a.weights[max(r[t], 0)];
+#pragma unroll
+    for (int t = 0; t < HELD; ++t) key[t] = r[t] < 0 ? 0u : order_of(w[t]);
+  }
+  // f(token, key) of the run's tokens; all of the wave's lanes come to it
+  auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < HELD; ++t)
+      if (t < chunks) f(first + 64 * t, key[t]);
+    for (int t = HELD; t < chunks; ++t) {
+      const int j = first + 64 * t, r = row_of(lo + min(j, n - 1));
+      f(j, r < 0 ? 0u : order_of(a.weights[r]));
     }
+  };
+  // sum of the waves before this one
+  auto before_wave = [&](const int* p) __attribute__((always_inline)) {
+    int s = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) s += w < wave ? p[w] : 0;
+    return s;
+  };
+
+  uint32_t top = 0;  // the digits found so far
+  int left = need;   // of the keys that have them, how many are chosen
+  uint32_t* const bins = hist + (lane & (kCopies - 1)) * kPitch;
+  for (int pass = 0; pass < 3 && need > 0; ++pass) {
+    const int at = pass == 0 ? 21 : pass == 1 ? 10 : 0, last = pass == 2 ? 1023 : 2047;
+    if (pass == 0)
+      each([&](int j, uint32_t k) __attribute__((always_inline)) {
+        if (j < n) atomicAdd(&bins[k >> 21], 1u);
+      });
+    else
+      each([&](int j, uint32_t k) __attribute__((always_inline)) {
+        if (j < n && k >> (pass == 1 ? 21 : 10) == top) atomicAdd(&bins[(k >> at) & last], 1u);
+      });
+    __syncthreads();
+    // thread t has bins 2 t', 2 t' + 1 with t' counted from the top; it leaves zeros
+    const int t = 1023 - tid;
+    int h0 = 0, h1 = 0;
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) {
+      uint2* const p = reinterpret_cast<uint2*>(&hist[c * kPitch + 2 * t]);
+      const uint2 h = *p;
+      *p = make_uint2(0, 0);
+      h0 += (int)h.x;
+      h1 += (int)h.y;
+    }
+    const int sum = lanes_up_to(h0 + h1);
     if (lane == 63) part[wave] = sum;
     __syncthreads();
-    uint32_t before = sum - h0 - h1;
-    for (int w = 0; w < wave; ++w) before += part[w];
+    const int before = sum - h0 - h1 + before_wave(part);
     // exactly one bin holds the left-th key from the top
-    if (before < (uint32_t)left && before + h1 >= (uint32_t)left) {
+    if (before < left && before + h1 >= left) {
       found = 2 * t + 1;
-      above = (int)before;
-    } else if (before + h1 < (uint32_t)left && before + h1 + h0 >= (uint32_t)left) {
+      above = before;
+    } else if (before + h1 < left && before + h1 + h0 >= left) {
       found = 2 * t;
-      above = (int)(before + h1);
+      above = before + h1;
     }
     __syncthreads();
     top = top << (pass == 2 ? 10 : 11) | (uint32_t)found;
@@ -99,38 +154,37 @@ __global__ __launch_bounds__(1024) void paged_choose_kernel(const PagedEvictArgs
     top = 0xffffffffu;
     left = 0;
   }
-  __syncthreads();
 
-  // runs of whole 64s
-  const int run = (n + 1023) / 1024 * 64, j0 = min(wave * run, n), j1 = min(j0 + run, n);
   int more = 0, same = 0;
-  for (int j = j0; j < j1; j += 64) {
-    const uint32_t k = j + lane < j1 ? key_of(j + lane) : 0;
-    more += __popcll(__ballot(j + lane < j1 && k > top));
-    same += __popcll(__ballot(j + lane < j1 && k == top));
+  each([&](int j, uint32_t k) __attribute__((always_inline)) {
+    if (j < n) {
+      more += k > top;
+      same += k == top;
+    }
+  });
+  more = lanes_up_to(more);
+  same = lanes_up_to(same);
+  __syncthreads();  // (the last pass's sums have been read)
+  if (lane == 63) {
+    part[wave] = more;
+    part_eq[wave] = same;
   }
-  if (lane == 0) waves[wave] = make_int2(more, same);
   __syncthreads();
-  more = same = 0;
-  for (int w = 0; w < wave; ++w) {
-    more += waves[w].x;
-    same += waves[w].y;
-  }
+  more = before_wave(part);
+  same = before_wave(part_eq);
   const uint64_t below = (1ull << lane) - 1;
   auto put = [&](int i, int j) __attribute__((always_inline)) {
     from[i] = row_of(j);
     if (kept) kept[i] = j;
   };
-  for (int j = j0; j < j1; j += 64) {
-    const bool in = j + lane < j1;
-    const uint32_t k = in ? key_of(j + lane) : 0;
-    const uint64_t gt = __ballot(in && k > top), eq = __ballot(in && k == top);
+  each([&](int j, uint32_t k) __attribute__((always_inline)) {
+    const uint64_t gt = __ballot(j < n && k > top), eq = __ballot(j < n && k == top);
     const int eq_before = same + __popcll(eq & below);
-    const bool take = in && (k > top || (k == top && eq_before < left));
-    if (take) put(lo + more + __popcll(gt & below) + min(eq_before, left), lo + j + lane);
+    if (j < n && (k > top || (k == top && eq_before < left)))
+      put(lo + more + __popcll(gt & below) + min(eq_before, left), lo + j);
     more += __popcll(gt);
     same += __popcll(eq);
-  }
+  });
   for (int i = tid; i < a.sinks; i += 1024) put(i, i);
   for (int i = tid; i < a.recent; i += 1024) put(a.keep - a.recent + i, hi + i);
 }
@@ -138,45 +192,69 @@ __global__ __launch_bounds__(1024) void paged_choose_kernel(const PagedEvictArgs
 // Token i of a list from page row from[i], in order: from[i] is that of a token
 // >= i, so a place is never read after a later step has written it, and within a
 // step everything is read before anything is written.  A workgroup moves a
-// column of the rows: COLUMN bytes of K or of V, the scales of one of them, or
-// the weights, so that the columns need not wait for each other.
-constexpr int kColumn = 128, kMoveThreads = 512, kMoveUnits = 4;
+// column of the rows: kColumn bytes of K or of V, the scales of one of them, or
+// the weights, so that the columns need not wait for each other.  The next
+// step's values are under way while this one's are stored (the places of this
+// step's tokens are behind it, the next step's come from further on), and the
+// places of the step after that.
+constexpr int kColumn = 128, kMoveThreads = 512;
+constexpr int kMoveUnits = 8;  // pieces of a thread and step
 template <typename U>
 RFX_DEV void move_column(const PagedEvictArgs& a, int b, const int32_t* from, int64_t hoff, char* base, int64_t row_bytes,
                          int lanes, int offset) {
-  const int tid = threadIdx.x, per = kMoveThreads / lanes;
+  const int tid = threadIdx.x, per = kMoveThreads / lanes, step = per * kMoveUnits;
   const int sub = tid / lanes, at = offset + (tid - sub * lanes) * (int)sizeof(U);
-  for (int i0 = 0; i0 < a.keep; i0 += per * kMoveUnits) {
-    U v[kMoveUnits];
-    char* to[kMoveUnits];
+  const int64_t table = (int64_t)b * a.q.max_pages;
+  const int slots = 1 << a.c.shift;
+  // what is behind the last token takes the last one's place, and is not stored
+  int src[2][kMoveUnits], page[2][kMoveUnits];
+  auto places = [&](int i0, int (&s)[kMoveUnits], int (&p)[kMoveUnits]) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < kMoveUnits; ++u) {
-      const int i = i0 + u * per + sub;
-      to[u] = nullptr;
-      v[u] = U{};
-      if (i >= a.keep) continue;
-      const int src = from[i];
-      int dst = page_row(a.c, a.q, b, i);
-      if (dst < 0) continue;
-      dst += (int)hoff;
-      if (src == dst) continue;
-      to[u] = base + (int64_t)dst * row_bytes + at;
-      if (src >= 0) v[u] = *reinterpret_cast<const U*>(base + (int64_t)src * row_bytes + at);
+      const int i = min(i0 + u * per + sub, a.keep - 1);
+      s[u] = from[i];
+      p[u] = a.q.table[table + (i >> a.c.shift)];  // (a sequence that is cut has a table for more than `keep`)
     }
+  };
+  U v[kMoveUnits], next[kMoveUnits];
+  auto load = [&](const int (&s)[kMoveUnits], U (&x)[kMoveUnits]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < kMoveUnits; ++u) {
+    for (int u = 0; u < kMoveUnits; ++u)
+      x[u] = *reinterpret_cast<const U*>(base + (int64_t)max(s[u], 0) * row_bytes + at);
+  };
+  places(0, src[0], page[0]);
+  places(step, src[1], page[1]);
+  load(src[0], v);
+  for (int i0 = 0; i0 < a.keep; i0 += step) {
+    int src2[kMoveUnits], page2[kMoveUnits];
+    load(src[1], next);
+    places(i0 + 2 * step, src2, page2);
+#pragma unroll
+    for (int u = 0; u < kMoveUnits; ++u) {  // this step's values are there
       if constexpr (sizeof(U) == 16) asm volatile("" : "+v"(v[u].x), "+v"(v[u].y), "+v"(v[u].z), "+v"(v[u].w));
       else asm volatile("" : "+v"(v[u]));
     }
-    __syncthreads();
+    asm volatile("s_barrier" ::: "memory");  // in every wave
 #pragma unroll
-    for (int u = 0; u < kMoveUnits; ++u)
-      if (to[u]) *reinterpret_cast<U*>(to[u]) = v[u];
+    for (int u = 0; u < kMoveUnits; ++u) {
+      const int i = i0 + u * per + sub;
+      const int dst = ((page[0][u] * a.c.n_kv) << a.c.shift) + (i & (slots - 1)) + (int)hoff;
+      if (i < a.keep && (unsigned)page[0][u] < (unsigned)a.c.n_pages && dst != src[0][u])
+        *reinterpret_cast<U*>(base + (int64_t)dst * row_bytes + at) = src[0][u] < 0 ? U{} : v[u];
+    }
+#pragma unroll
+    for (int u = 0; u < kMoveUnits; ++u) {
+      v[u] = next[u];
+      src[0][u] = src[1][u];
+      page[0][u] = page[1][u];
+      src[1][u] = src2[u];
+      page[1][u] = page2[u];
+    }
   }
 }
 
-__global__ __launch_bounds__(kMoveThreads) void paged_move_kernel(const PagedEvictArgs a, int row_bytes, int columns, int scaled) {
-  const int all = 2 * columns + 2 * scaled + 1;
+__global__ __launch_bounds__(kMoveThreads) void paged_move_kernel(const PagedEvictArgs a, int row_bytes, int column, int scaled) {
+  const int columns = row_bytes / column, all = 2 * columns + 2 * scaled + 1;
   const int64_t list = blockIdx.x / all;
   const int col = blockIdx.x - (int)list * all;
   const int b = (int)(list / a.c.n_kv), g = (int)(list - (int64_t)b * a.c.n_kv);
@@ -187,7 +265,7 @@ __global__ __launch_bounds__(kMoveThreads) void paged_move_kernel(const PagedEvi
   const int64_t hoff = (int64_t)g << a.c.shift;
   if (col < 2 * columns) {
     const int side = col / columns, x = col - side * columns;
-    move_column<uint4>(a, b, from, hoff, side ? a.c.v : a.c.k, row_bytes, min(row_bytes, kColumn) / 16, x * kColumn);
+    move_column<uint4>(a, b, from, hoff, side ? a.c.v : a.c.k, row_bytes, column / 16, x * column);
   } else if (col < all - 1) {
     move_column<float>(a, b, from, hoff, reinterpret_cast<char*>(col == 2 * columns ? a.c.k_scale : a.c.v_scale), 4, 1, 0);
   } else {
@@ -202,13 +280,16 @@ __global__ __launch_bounds__(kMoveThreads) void paged_move_kernel(const PagedEvi
 
 }  // namespace
 
-hipError_t launch_paged_evict(const PagedEvictArgs& a, int elem_bytes, int scaled, hipStream_t s) {
-  RFX_LAUNCH(paged_choose_kernel, dim3((unsigned)(a.c.n_kv * a.q.n)), dim3(1024), 0, s, a);
+hipError_t launch_paged_evict(const PagedEvictArgs& a, int elem_bytes, int scaled, int64_t keys, hipStream_t s) {
+  const dim3 lists((unsigned)(a.c.n_kv * a.q.n));
+  if (keys <= 4096) RFX_LAUNCH(paged_choose_kernel<4>, lists, dim3(1024), 0, s, a);
+  else if (keys <= 16384) RFX_LAUNCH(paged_choose_kernel<16>, lists, dim3(1024), 0, s, a);
+  else RFX_LAUNCH(paged_choose_kernel<32>, lists, dim3(1024), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int row_bytes = a.c.dh * elem_bytes, columns = row_bytes < kColumn ? 1 : row_bytes / kColumn;
-  const int64_t blocks = (int64_t)a.q.n * a.c.n_kv * (2 * columns + 2 * scaled + 1);
-  RFX_LAUNCH(paged_move_kernel, dim3((unsigned)blocks), dim3(kMoveThreads), 0, s, a, row_bytes, columns, scaled);
+  const int row_bytes = a.c.dh * elem_bytes, column = std::min(row_bytes, kColumn);
+  const dim3 grid((unsigned)((int64_t)a.q.n * a.c.n_kv * (2 * (row_bytes / column) + 2 * scaled + 1)));
+  RFX_LAUNCH(paged_move_kernel, grid, dim3(kMoveThreads), 0, s, a, row_bytes, column, scaled);
   return hipGetLastError();
 }
 
