@@ -666,11 +666,13 @@ int reflex_paged_tree(const reflex_paged_batch* batch, const int32_t* parents, i
                       int32_t mask_words, int64_t* positions, void* stream);
 
 /*
- * Attention of drafted tokens: as reflex_paged_attention, in each respect and
- * with its workspace, where row r sees the present tokens before its sequence's
+ * Attention of drafted tokens: as reflex_paged_attention in each respect, with a
+ * workspace of its own size, where row r sees the present tokens before its sequence's
  * rows (j < lengths[b] - n_b) and those of the sequence's rows that its bits
  * name.  A row may see nothing, itself included: then it gets zeros.
  */
+int reflex_paged_tree_attention_workspace(const reflex_paged_cache* cache, const reflex_paged_batch* batch,
+                                          int64_t n_rows, int32_t n_q_heads, int32_t dtype, size_t* bytes);
 int reflex_paged_tree_attention(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const reflex_rows* q,
                                 const reflex_rows* out, int64_t n_rows, int32_t n_q_heads, int32_t dtype, float scale,
                                 const uint64_t* mask, int32_t mask_words, void* workspace, size_t workspace_bytes,

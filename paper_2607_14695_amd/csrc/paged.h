@@ -58,6 +58,26 @@ RFX_DEV int page_row(const Pages& c, const Seqs& q, int b, int64_t pos) {
   return ((page * c.n_kv) << c.shift) + (int)(pos & ((1 << c.shift) - 1));
 }
 
+// Sum of a value over the lanes up to this one: within 16 lanes, then across them.
+RFX_DEV int lanes_up_to(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15, 31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+
+// r / d for 0 <= r <= 2^30 with a quotient below 2^23, given 1 / d: the product is
+// off by less than one.
+RFX_DEV int divided(int r, int d, float inv) {
+  int q = (int)((float)r * inv);
+  const int rest = r - q * d;
+  q += rest >= d ? 1 : 0;
+  return q - (rest < 0 ? 1 : 0);
+}
+
 struct RotaryArgs {
   const int64_t* pos;   // [axis * ps + row]; null: the token's index (writes only)
   int64_t ps;
@@ -106,6 +126,7 @@ struct PagedAttnArgs {
   float2* part_ml;   // [n_rows * n_q][nsplit] (running maximum, sum)
   const uint64_t* tree;  // kTree: [n_rows][tree_words], which of its sequence's rows a row sees
   int tree_words;
+  int units, tile_rows;  // kTree: workgroups of a K/V head that the chip holds, rows of a tile; nsplit: at most
   float2* stats;     // kWeigh: [n_rows * n_q] (maximum, 1 / sum, or 0 for a row that sees nothing)
   float* scores;     // kWeigh: [n_rows * n_q][score_pitch] in units of log2 e, if row_splits is 0; else the
                      // row splits' sums [row_splits][sequences * K/V heads][score_pitch]
@@ -118,6 +139,11 @@ struct PagedAttnPlan {
 };
 PagedAttnPlan paged_attention_plan(const reflex_paged_cache& c, const reflex_paged_batch& b, int64_t n_rows, int n_q,
                                    int dtype, int window);
+struct PagedTreePlan {
+  int tile_rows, units, nsplit;
+  size_t bytes;
+};
+PagedTreePlan paged_tree_plan(const reflex_paged_cache& c, const reflex_paged_batch& b, int64_t n_rows, int n_q, int dtype);
 // How weighed attention comes to the keys' sums: from kept scores (row_splits
 // 0), or from scores that are formed again by so many workgroups for the same keys.
 struct PagedWeighPlan {

@@ -116,8 +116,7 @@ int check_attention(const reflex_rows* q, const reflex_rows* out, int64_t n_rows
 
 void fill_attention(PagedAttnArgs& a, const reflex_paged_cache* cache, const reflex_paged_batch* batch,
                     const reflex_rows* q, const reflex_rows* out, int64_t n_rows, int32_t n_q_heads, int32_t dtype,
-                    float scale, int32_t causal, int32_t window, void* workspace) {
-  const PagedAttnPlan p = paged_attention_plan(*cache, *batch, n_rows, n_q_heads, dtype, window);
+                    float scale, int32_t causal, int32_t window, int nsplit, void* workspace) {
   a.c = pages_of(cache);
   a.q = seqs_of(batch);
   a.x = rows_of(q);
@@ -131,12 +130,14 @@ void fill_attention(PagedAttnArgs& a, const reflex_paged_cache* cache, const ref
   a.factor = (scale < 0.f ? -1.f : 1.f) * (s2 < tiny ? 0x1p-64f : 1.f);
   a.causal = causal != 0;
   a.window = window;
-  a.nsplit = p.nsplit;
-  const size_t rows = (size_t)n_rows * n_q_heads * p.nsplit;
+  a.nsplit = nsplit;
+  const size_t rows = (size_t)n_rows * n_q_heads * nsplit;
   a.part_o = reinterpret_cast<float*>(workspace);
   a.part_ml = reinterpret_cast<float2*>(reinterpret_cast<char*>(workspace) + rows * cache->head_dim * sizeof(float));
   a.tree = nullptr;
   a.tree_words = 0;
+  a.units = 0;
+  a.tile_rows = 0;
   a.stats = nullptr;
   a.scores = nullptr;
   a.score_pitch = 0;
@@ -275,7 +276,8 @@ int reflex_paged_attention(const reflex_paged_cache* cache, const reflex_paged_b
   PagedAttnArgs a;
   RFX_CHECK(check_attention(q, out, n_rows, dtype, scale, window, workspace, workspace_bytes, need));
   if (n_rows == 0 || batch->n_seqs == 0) return REFLEX_OK;
-  fill_attention(a, cache, batch, q, out, n_rows, n_q_heads, dtype, scale, causal, window, workspace);
+  fill_attention(a, cache, batch, q, out, n_rows, n_q_heads, dtype, scale, causal, window,
+                 paged_attention_plan(*cache, *batch, n_rows, n_q_heads, dtype, window).nsplit, workspace);
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   return done(dtype == REFLEX_DTYPE_BF16 ? launch_paged_attention<bf16_t>(a, cache->store, s)
                                          : launch_paged_attention<float>(a, cache->store, s));
@@ -292,20 +294,30 @@ int reflex_paged_tree(const reflex_paged_batch* batch, const int32_t* parents, i
   return done(launch_paged_tree(a, reinterpret_cast<hipStream_t>(stream)));
 }
 
+int reflex_paged_tree_attention_workspace(const reflex_paged_cache* cache, const reflex_paged_batch* batch,
+                                          int64_t n_rows, int32_t n_q_heads, int32_t dtype, size_t* bytes) {
+  RFX_CHECK(reflex_paged_attention_workspace(cache, batch, n_rows, n_q_heads, dtype, bytes));
+  if (n_rows > 0 && batch->n_seqs > 0) *bytes = paged_tree_plan(*cache, *batch, n_rows, n_q_heads, dtype).bytes;
+  return REFLEX_OK;
+}
+
 int reflex_paged_tree_attention(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const reflex_rows* q,
                                 const reflex_rows* out, int64_t n_rows, int32_t n_q_heads, int32_t dtype, float scale,
                                 const uint64_t* mask, int32_t mask_words, void* workspace, size_t workspace_bytes,
                                 void* stream) {
   size_t need = 0;
-  RFX_CHECK(reflex_paged_attention_workspace(cache, batch, n_rows, n_q_heads, dtype, &need));
+  RFX_CHECK(reflex_paged_tree_attention_workspace(cache, batch, n_rows, n_q_heads, dtype, &need));
   RFX_CHECK(check_words(mask_words));
   PagedAttnArgs a;
   RFX_CHECK(check_attention(q, out, n_rows, dtype, scale, 0, workspace, workspace_bytes, need));
   if (n_rows == 0 || batch->n_seqs == 0) return REFLEX_OK;
   if (!mask || ((uintptr_t)mask & 7)) return REFLEX_EINVAL;
-  fill_attention(a, cache, batch, q, out, n_rows, n_q_heads, dtype, scale, 0, 0, workspace);
+  const PagedTreePlan p = paged_tree_plan(*cache, *batch, n_rows, n_q_heads, dtype);
+  fill_attention(a, cache, batch, q, out, n_rows, n_q_heads, dtype, scale, 0, 0, p.nsplit, workspace);
   a.tree = mask;
   a.tree_words = mask_words;
+  a.units = p.units;
+  a.tile_rows = p.tile_rows;
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   return done(dtype == REFLEX_DTYPE_BF16 ? launch_paged_tree_attention<bf16_t>(a, cache->store, s)
                                          : launch_paged_tree_attention<float>(a, cache->store, s));
@@ -344,7 +356,8 @@ int reflex_paged_weighed_attention(const reflex_paged_cache* cache, const reflex
   RFX_CHECK(check_attention(q, out, n_rows, dtype, scale, window, workspace, workspace_bytes, need));
   if (n_rows == 0 || batch->n_seqs == 0) return REFLEX_OK;
   if (!weights || ((uintptr_t)weights & 3)) return REFLEX_EINVAL;
-  fill_attention(a, cache, batch, q, out, n_rows, n_q_heads, dtype, scale, causal, window, workspace);
+  fill_attention(a, cache, batch, q, out, n_rows, n_q_heads, dtype, scale, causal, window,
+                 paged_attention_plan(*cache, *batch, n_rows, n_q_heads, dtype, window).nsplit, workspace);
   char* const stats = reinterpret_cast<char*>(workspace) + whole_256(part);
   a.stats = reinterpret_cast<float2*>(stats);
   const PagedWeighPlan p = paged_weigh_plan(*cache, *batch, n_rows, n_q_heads, dtype);

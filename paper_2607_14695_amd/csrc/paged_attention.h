@@ -349,6 +349,91 @@ RFX_DEV int count_tiles(const PagedAttnArgs& a, int bm, int lane) {
   return __builtin_amdgcn_readfirstlane(sum);
 }
 
+// kTree: trees are small, and the sequences below them differ in length, so tiles
+// are not split alike: the batch's work (tiles x keys) is divided by the number of
+// workgroups that the chip holds, and every tile has as many splits, alike ones, as
+// that many keys to a split ask for.  32 ragged trees of 26 to 64 rows of 8 heads over 3,000 to
+// 15,409 fp8 keys took 327 us with two splits each (the longest ones' time).
+//
+// A unit is a tile's split; units are numbered over the sequences, in each over
+// the splits and in these over the tiles, which share the split's keys.
+struct Units { int per, total; };  // keys of a split, units of a K/V head
+struct UnitSeq { int c0, c1, end, len, tiles, keys; };
+RFX_DEV UnitSeq unit_seq(const PagedAttnArgs& a, int b, int bm) {
+  UnitSeq s{0, 0, 0, 0, 0, 0};
+  if (b < a.q.n) {
+    s.c0 = (int)min((int64_t)max(a.q.cu[b], 0), a.n_rows);
+    s.end = a.q.cu[b + 1];
+    s.c1 = (int)min((int64_t)max(s.end, 0), a.n_rows);
+    s.len = a.q.len[b];
+    s.tiles = s.c1 > s.c0 ? ((s.c1 - s.c0) * a.group + bm - 1) / bm : 0;
+    s.keys = max(min(s.len, a.q.max_pages << a.c.shift), 1);  // (a table holds 2^30 tokens at most)
+  }
+  return s;
+}
+RFX_DEV int lanes_sum(int x) { return __builtin_amdgcn_readlane(lanes_up_to(x), 63); }
+RFX_DEV Units count_units(const PagedAttnArgs& a, int bm, int lane, const UnitSeq& first) {
+  // in units of 128 keys, of which 2^23 rows in tiles of 16 over 2^30 keys make less than 2^43
+  int64_t work = 0;
+  int longest = 0;
+  for (int b0 = 0; b0 < a.q.n; b0 += 64) {
+    const UnitSeq s = b0 ? unit_seq(a, b0 + lane, bm) : first;
+    const int k = (s.keys + 127) >> 7;
+    const int64_t x = (int64_t)s.tiles * k;
+    work += (int64_t)lanes_sum((int)(x & 0xfffff)) + ((int64_t)lanes_sum((int)(x >> 20)) << 20);
+    int m = s.tiles ? k : 0;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = max(m, __shfl_xor(m, o, 64));
+    longest = max(longest, __builtin_amdgcn_readfirstlane(m));
+  }
+  // keys of a split in 128s, at first
+  int64_t per = max(max((work + a.units - 1) / a.units, (int64_t)((longest + a.nsplit - 1) / a.nsplit)), (int64_t)1);
+  Units u;
+  // (each tile's last split may be short: once more with what there then are too many)
+  for (int turn = 0;; ++turn) {
+    u.per = __builtin_amdgcn_readfirstlane((int)min(per * 128, (int64_t)1 << 30));
+    u.total = 0;
+    const float inv = 1.f / (float)u.per;
+    for (int b0 = 0; b0 < a.q.n; b0 += 64) {
+      const UnitSeq s = b0 ? unit_seq(a, b0 + lane, bm) : first;
+      u.total += lanes_sum(s.tiles * (s.tiles ? divided(s.keys - 1, u.per, inv) + 1 : 0));
+    }
+    if (turn == 2 || u.total <= a.units || per >= longest) return u;
+    per = max(per + 1, (per * u.total + a.units - 1) / a.units);
+  }
+}
+// `splits`: how many the tile has; `part`: the unit's keys, of those that any row may see.
+RFX_DEV bool find_unit(const PagedAttnArgs& a, int unit, int bm, int lane, const UnitSeq& first, int per, Tile& t,
+                       int& split, int& splits, Span& part) {
+  int before = 0;
+  const float inv = 1.f / (float)per;
+  for (int b0 = 0; b0 < a.q.n; b0 += 64) {
+    const UnitSeq s = b0 ? unit_seq(a, b0 + lane, bm) : first;
+    const int ns = s.tiles ? divided(s.keys - 1, per, inv) + 1 : 0, mine = s.tiles * ns, sum = lanes_up_to(mine);
+    const uint64_t past = __ballot(before + sum > unit);
+    if (past) {
+      const int src = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)past) - 1);
+      auto of = [&](int v) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(v, src); };
+      const int local = unit - before - (of(sum) - of(mine)), tiles = of(s.tiles);
+      split = __builtin_amdgcn_readfirstlane(local / tiles);
+      splits = of(ns);
+      const int keys = of(s.keys);
+      const int alike = __builtin_amdgcn_readfirstlane((keys + 128 * splits - 1) / (128 * splits) * 128);
+      part.lo = min(split * alike, keys);
+      part.hi = min(part.lo + alike, keys);
+      t.b = b0 + src;
+      t.r0 = __builtin_amdgcn_readfirstlane((local - split * tiles) * bm);
+      t.first_row = of(s.c0);
+      t.rows = (of(s.c1) - of(s.c0)) * a.group;
+      t.len = of(s.len);
+      t.first_pos = (int)((int64_t)t.len - of(s.end) + of(s.c0));
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(sum, 63);
+  }
+  return false;
+}
+
 // Row `q` of a tile done again where its result is not finite: key by key, which
 // reads only what the row sees.  Needed where a key that this row does not see,
 // but another row of the tile does, has a value that is not finite, which has met
@@ -370,12 +455,21 @@ RFX_DEV void redo_row(int tile, int bm, int q, int64_t row, int head, int split,
   uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
   asm volatile("" : "+s"(at));
   const PagedAttnArgs& a = *reinterpret_cast<const PagedAttnArgs*>(at);
+  const int lane = threadIdx.x & 63;
   Tile t;
-  if (!find_tile(a, tile, bm, threadIdx.x & 63, t)) return;
+  Span part;
+  if constexpr (MODE == kTree) {
+    const UnitSeq first = unit_seq(a, lane, bm);
+    const int per = count_units(a, bm, lane, first).per;
+    int splits;
+    if (!find_unit(a, tile, bm, lane, first, per, t, split, splits, part)) return;
+  } else {
+    if (!find_tile(a, tile, bm, lane, t)) return;
+  }
   const int last = min(bm, t.rows - t.r0) - 1;
   const Span first_sees = span_of(a, t.first_pos + t.r0 / a.group, t.len);
   const Span last_sees = span_of(a, t.first_pos + (t.r0 + last) / a.group, t.len);
-  const Span part = split_of(a, first_sees.lo, last_sees.hi, split);
+  if constexpr (MODE != kTree) part = split_of(a, first_sees.lo, last_sees.hi, split);
   Span sp = span_of(a, t.first_pos + (t.r0 + q) / a.group, t.len);
   sp.lo = max(sp.lo, part.lo);
   sp.hi = min(sp.hi, part.hi);
@@ -390,7 +484,7 @@ RFX_DEV void redo_row(int tile, int bm, int q, int64_t row, int head, int split,
 // not finite a score that the row does see was not, and all of the row is NaN.
 template <int MODE, typename T, int ST, int DH>
 RFX_DEV void finish_row(const PagedAttnArgs& a, int tile, int bm, int q, int64_t row, int head, int split, bool halves,
-                        float M, float L, float* y) {
+                        float M, float L, float* y, int splits = 0) {
   constexpr int N = DH / 64;
   if constexpr (ST != REFLEX_STORE_INT8) {
     bool odd = false;
@@ -407,6 +501,8 @@ RFX_DEV void finish_row(const PagedAttnArgs& a, int tile, int bm, int q, int64_t
   }
   const int64_t at = (row * a.n_q + head) * a.nsplit + split;
   if (lane == 0) a.part_ml[at] = make_float2(M, L);
+  // (splits that the tile does not have)
+  if (MODE == kTree && split == 0 && lane >= splits && lane < a.nsplit) a.part_ml[at + lane] = make_float2(kFloor, 0.f);
   if (L == 0.f) return;
   float* p = a.part_o + at * DH + lane * N;
 #pragma unroll
@@ -472,9 +568,17 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, c16 = lane & 15;
-  const int kvh = blockIdx.y / a.nsplit, split = blockIdx.y - kvh * a.nsplit;
+  const int kvh = MODE == kTree ? blockIdx.y : blockIdx.y / a.nsplit;
+  int split = MODE == kTree ? 0 : blockIdx.y - kvh * a.nsplit, splits = 0;
+  Span part;
   Tile t;
-  if (!find_tile(a, blockIdx.x, BM, lane, t)) return;
+  if constexpr (MODE == kTree) {
+    const UnitSeq first = unit_seq(a, lane, BM);
+    const int per = count_units(a, BM, lane, first).per;
+    if (!find_unit(a, blockIdx.x, BM, lane, first, per, t, split, splits, part)) return;
+  } else {
+    if (!find_tile(a, blockIdx.x, BM, lane, t)) return;
+  }
 
   // keys that any row of the tile sees, cut to this split
   const int rows_here = min(BM, t.rows - t.r0);
@@ -483,7 +587,8 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
   const int lo_max = span_of(a, p1, t.len).lo;
   // (in a tree every row sees the cached tokens)
   const int hi_min = MODE == kTree ? min(t.first_pos, hi_max) : span_of(a, p0, t.len).hi;
-  const Span part = split_of(a, lo_min, hi_max, split);
+  if constexpr (MODE == kTree) part.hi = min(part.hi, hi_max);
+  else part = split_of(a, lo_min, hi_max, split);
   const int k_beg = part.lo, k_end = part.hi;
 
   // query rows: column c16 of block m
@@ -873,7 +978,7 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
     }
     const int r = t.r0 + q, tok = r / a.group, head = kvh * a.group + (r - tok * a.group);
     const int64_t row = t.first_row + tok;
-    finish_row<MODE, T, ST, DH>(a, blockIdx.x, BM, q, row, head, split, BF, M, L, y);
+    finish_row<MODE, T, ST, DH>(a, blockIdx.x, BM, q, row, head, split, BF, M, L, y, splits);
   }
 }
 
@@ -940,20 +1045,34 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
   // that the batch has, not of the grid's: with those a chunk of 1,024 rows of 8
   // heads over 8,192 keys gave some XCDs one too many and took 159 us instead of
   // 93 (now 88).  (Narrower heads, two workgroups to a CU, lose 2 % to the counting.)
-  const int tiles = WIDE ? count_tiles(a, BM, lane) : grid_tiles;
-  const int all = tiles * a.c.n_kv * a.nsplit, per = (all + 7) >> 3;
+  int split, splits = 0;
+  UnitSeq first;
+  Units units;
+  if constexpr (MODE == kTree) {
+    first = unit_seq(a, lane, BM);
+    units = count_units(a, BM, lane, first);
+  }
+  const int tiles = MODE == kTree ? units.total : WIDE ? count_tiles(a, BM, lane) : grid_tiles;
+  const int all = tiles * a.c.n_kv * (MODE == kTree ? 1 : a.nsplit), per = (all + 7) >> 3;
   const int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
   if ((int)(blockIdx.x >> 3) >= per || id >= all) return;
   const int grp = id / tiles;
-  const int kvh = grp / a.nsplit, split = grp - kvh * a.nsplit;
+  const int kvh = MODE == kTree ? __builtin_amdgcn_readfirstlane(grp) : grp / a.nsplit;
+  if constexpr (MODE != kTree) split = grp - kvh * a.nsplit;
   Tile t;
-  const int tile = tiles - 1 - (id - grp * tiles);
-  if (!find_tile(a, tile, BM, lane, t)) return;
+  Span part;
+  const int tile = MODE == kTree ? id - grp * tiles : tiles - 1 - (id - grp * tiles);
+  if constexpr (MODE == kTree) {
+    if (!find_unit(a, tile, BM, lane, first, units.per, t, split, splits, part)) return;
+  } else {
+    if (!find_tile(a, tile, BM, lane, t)) return;
+  }
 
   const int rows_here = min(BM, t.rows - t.r0);
   const int p0 = t.first_pos + t.r0 / a.group, p1 = t.first_pos + (t.r0 + rows_here - 1) / a.group;
   const Span sp0 = span_of(a, p0, t.len), sp1 = span_of(a, p1, t.len);
-  const Span part = split_of(a, sp0.lo, sp1.hi, split);
+  if constexpr (MODE == kTree) part.hi = min(part.hi, sp1.hi);
+  else part = split_of(a, sp0.lo, sp1.hi, split);
   const int k_beg = part.lo, k_end = part.hi;
 
   const int r = t.r0 + 32 * wave + r32;
@@ -1359,7 +1478,7 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
 #pragma unroll
     for (int i = 0; i < N; ++i) y[i] = ex[q * OP + lane * N + i];
     finish_row<MODE, T, ST, DH>(a, tile, BM, 32 * wave + q, t.first_row + tq, kvh * a.group + (rq - tq * a.group), split, false,
-                          w.x, w.y, y);
+                          w.x, w.y, y, splits);
   }
 }
 
@@ -1376,15 +1495,21 @@ __global__ __launch_bounds__(256) void paged_attn_merge_kernel(const PagedAttnAr
   if (row >= a.n_rows) return;
   const float* p = a.part_o + id * a.nsplit * DH + lane * N;
   float v[G][N];
+  int splits = a.nsplit;
   auto request = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < G; ++u)
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[u][i] = p[(int64_t)min(s0 + u, a.nsplit - 1) * DH + i];
+      for (int i = 0; i < N; ++i)
+        if (MODE != kTree || s0 + u < splits) v[u][i] = p[(int64_t)min(s0 + u, splits - 1) * DH + i];
   };
-  request(0);
+  if constexpr (MODE != kTree) request(0);
   const float2 w = lane < a.nsplit ? a.part_ml[id * a.nsplit + lane] : make_float2(kFloor, 0.f);
   if (row < a.q.cu[0] || row >= a.q.cu[a.q.n]) return;
+  if constexpr (MODE == kTree) {  // a tile may have few of the splits that there is room for
+    splits = max(64 - (int)__clzll(__ballot(w.y != 0.f)), 1);
+    request(0);
+  }
   float M = w.x;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
@@ -1433,13 +1558,16 @@ inline int rows_of_tile(int64_t n_rows, int n_seqs, int group, int n_kv, int dh,
 
 template <int MODE, typename T, int ST, int DH>
 hipError_t launch_shape(const PagedAttnArgs& a, hipStream_t s) {
-  const int bm = rows_of_tile(a.n_rows, a.q.n, a.group, a.c.n_kv, DH,
-                              sizeof(T) == 2 ? REFLEX_DTYPE_BF16 : REFLEX_DTYPE_F32);
-  const int64_t tiles = tile_bound(a.n_rows, a.q.n, a.group, bm);
-  const dim3 grid((unsigned)tiles, (unsigned)(a.c.n_kv * a.nsplit));
+  const int bm = MODE == kTree ? a.tile_rows
+                               : rows_of_tile(a.n_rows, a.q.n, a.group, a.c.n_kv, DH,
+                                              sizeof(T) == 2 ? REFLEX_DTYPE_BF16 : REFLEX_DTYPE_F32);
+  // (units: what the division gives, and a short last split of every tile)
+  const int64_t tiles = tile_bound(a.n_rows, a.q.n, a.group, bm) + (MODE == kTree ? a.units : 0);
+  const int splits = MODE == kTree ? 1 : a.nsplit;
+  const dim3 grid((unsigned)tiles, (unsigned)(a.c.n_kv * splits));
   if constexpr (sizeof(T) == 2 && MODE != kKept) {
     if (bm == 128) {
-      const unsigned n = (unsigned)((tiles * a.c.n_kv * a.nsplit + 7) / 8 * 8);
+      const unsigned n = (unsigned)((tiles * a.c.n_kv * splits + 7) / 8 * 8);
       RFX_LAUNCH((paged_attn_many_kernel<MODE, ST, DH>), dim3(n), dim3(256), 0, s, a, (int)tiles);
     }
   }

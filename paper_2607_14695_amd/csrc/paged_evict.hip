@@ -24,17 +24,6 @@ constexpr int kCopies = 4;        // of the histogram: a lane adds to copy lane 
 constexpr int kPitch = kBins + 16;  // equal digits; the copies' equal bins lie in different banks
 constexpr int kTable = 4096;      // table entries held in LDS, if that is all of them
 
-// Sum of a value over the lanes up to this one: within 16 lanes, then across them.
-RFX_DEV int lanes_up_to(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr 1, 2, 4, 8
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15, 31
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-  return x;
-}
-
 // The least of the `need` greatest keys is found digit by digit (11, 11 and 10
 // bits): a histogram of the digits of those keys that agree so far, summed from
 // the top.  Counts are whole numbers, so the order of the additions does not

@@ -54,24 +54,35 @@ __global__ __launch_bounds__(256) void paged_tree_kernel(const PagedTreeArgs a) 
 // + path[i].  Both go up and path[i] >= i, so a place is never read after a
 // later step has written it: the workgroup takes the moves in order, some
 // thousands of bytes a step, and stores a step only when all of it was read.
-// One workgroup to a sequence, which also writes its length.
+// One workgroup to a sequence, which also writes its length (32 sequences of 6
+// tokens of one 256-wide head 3.7 us, a chain of latencies); where that would be
+// many bytes, one to each `per_part` heads, and the lengths in a launch of their
+// own (8 sequences of up to 90 tokens of 8 heads of 128 took 31 us in 8
+// workgroups).
+struct Accepted { int64_t n, first; int c; };
+RFX_DEV Accepted accepted_of(const PagedAcceptArgs& a, int b) {
+  Accepted x;
+  x.n = max((int64_t)a.q.cu[b + 1] - a.q.cu[b], (int64_t)0);
+  x.first = (int64_t)a.q.len[b] - x.n;
+  x.c = (int)min((int64_t)max(a.counts[b], 0), min(x.n, (int64_t)a.max_path));
+  return x;
+}
+
 constexpr int kAcceptUnits = 4;  // 16-byte pieces of a thread and step
-__global__ __launch_bounds__(1024) void paged_accept_kernel(const PagedAcceptArgs a, int row_bytes, int scaled) {
-  const int b = blockIdx.x;
-  const int len = a.q.len[b];
-  const int64_t n = max((int64_t)a.q.cu[b + 1] - a.q.cu[b], (int64_t)0);
-  const int64_t first = (int64_t)len - n;
-  const int c = (int)min((int64_t)max(a.counts[b], 0), min(n, (int64_t)a.max_path));
+__global__ __launch_bounds__(1024) void paged_accept_kernel(const PagedAcceptArgs a, int row_bytes, int scaled, int per_part) {
+  const int parts = (a.c.n_kv + per_part - 1) / per_part;
+  const int b = blockIdx.x / parts, h0 = (blockIdx.x - b * parts) * per_part, heads = min(per_part, a.c.n_kv - h0);
+  const Accepted x = accepted_of(a, b);
   const int32_t* const path = a.path + (int64_t)b * a.max_path;
   // (page row of head 0 that accepted token i comes from, and goes to)
   auto places = [&](int i, int& src, int& dst) __attribute__((always_inline)) {
     const int p = path[i];
-    dst = page_row(a.c, a.q, b, first + i);
-    src = p < 0 || p >= n ? -1 : page_row(a.c, a.q, b, first + p);
+    dst = page_row(a.c, a.q, b, x.first + i);
+    src = p < 0 || p >= x.n ? -1 : page_row(a.c, a.q, b, x.first + p);
   };
   const int per_row = row_bytes / 16;
-  const int units = 2 * a.c.n_kv * per_row;  // of a token: K and V of every head
-  const int64_t all = (int64_t)c * units;
+  const int units = 2 * heads * per_row;  // of a token: K and V of the heads
+  const int64_t all = (int64_t)x.c * units;
   for (int64_t e0 = 0; e0 < all; e0 += 1024 * kAcceptUnits) {
     uint4 v[kAcceptUnits];
     char* to[kAcceptUnits];
@@ -82,13 +93,13 @@ __global__ __launch_bounds__(1024) void paged_accept_kernel(const PagedAcceptArg
       v[u] = zero16();
       if (e >= all) continue;
       const int i = (int)(e / units), w = (int)(e - (int64_t)i * units);
-      const int side = w / (units / 2), x = w - side * (units / 2);
-      const int h = x / per_row, piece = x - h * per_row;
+      const int side = w / (units / 2), y = w - side * (units / 2);
+      const int h = y / per_row, piece = y - h * per_row;
       int src, dst;
       places(i, src, dst);
       if (dst < 0 || src == dst) continue;
       char* const base = side ? a.c.v : a.c.k;
-      const int64_t hoff = (int64_t)h << a.c.shift;
+      const int64_t hoff = (int64_t)(h0 + h) << a.c.shift;
       to[u] = base + (dst + hoff) * row_bytes + piece * 16;
       if (src >= 0) v[u] = ld16(base + (src + hoff) * row_bytes + piece * 16);
     }
@@ -100,8 +111,8 @@ __global__ __launch_bounds__(1024) void paged_accept_kernel(const PagedAcceptArg
       if (to[u]) st16(to[u], v[u]);
   }
   if (scaled) {
-    const int per = 2 * a.c.n_kv;
-    const int64_t total = (int64_t)c * per;
+    const int per = 2 * heads;
+    const int64_t total = (int64_t)x.c * per;
     for (int64_t e0 = 0; e0 < total; e0 += 1024) {
       const int64_t e = e0 + threadIdx.x;
       float v = 0.f;
@@ -111,7 +122,7 @@ __global__ __launch_bounds__(1024) void paged_accept_kernel(const PagedAcceptArg
         int src, dst;
         places(i, src, dst);
         if (dst >= 0 && src != dst) {
-          float* const base = (w >= a.c.n_kv ? a.c.v_scale : a.c.k_scale) + ((int64_t)(w % a.c.n_kv) << a.c.shift);
+          float* const base = (w >= heads ? a.c.v_scale : a.c.k_scale) + ((int64_t)(h0 + w % heads) << a.c.shift);
           to = base + dst;
           if (src >= 0) v = base[src];
         }
@@ -121,8 +132,16 @@ __global__ __launch_bounds__(1024) void paged_accept_kernel(const PagedAcceptArg
       if (to) *to = v;
     }
   }
+  if (parts > 1) return;
   __syncthreads();  // every thread has read the length
-  if (threadIdx.x == 0) a.lengths[b] = (int32_t)max(first + c, (int64_t)0);
+  if (threadIdx.x == 0) a.lengths[b] = (int32_t)max(x.first + x.c, (int64_t)0);
+}
+
+__global__ __launch_bounds__(256) void paged_accepted_lengths_kernel(const PagedAcceptArgs a) {
+  const int b = blockIdx.x * 256 + threadIdx.x;
+  if (b >= a.q.n) return;
+  const Accepted x = accepted_of(a, b);
+  a.lengths[b] = (int32_t)max(x.first + x.c, (int64_t)0);
 }
 
 }  // namespace
@@ -133,8 +152,47 @@ hipError_t launch_paged_tree(const PagedTreeArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_paged_accept(const PagedAcceptArgs& a, int elem_bytes, int scaled, hipStream_t s) {
-  RFX_LAUNCH(paged_accept_kernel, dim3((unsigned)a.q.n), dim3(1024), 0, s, a, a.c.dh * elem_bytes, scaled);
-  return hipGetLastError();
+  const int row_bytes = a.c.dh * elem_bytes;
+  // a step of a workgroup is 64 KB
+  const int64_t bytes = 2ll * a.max_path * a.c.n_kv * row_bytes;
+  const int parts = (int)std::min<int64_t>(a.c.n_kv, std::max<int64_t>(1, std::min<int64_t>(bytes >> 16, 2048 / a.q.n)));
+  const int per_part = (a.c.n_kv + parts - 1) / parts, grid = a.q.n * ((a.c.n_kv + per_part - 1) / per_part);
+  RFX_LAUNCH(paged_accept_kernel, dim3((unsigned)grid), dim3(1024), 0, s, a, row_bytes, scaled, per_part);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && grid > a.q.n) {
+    RFX_LAUNCH(paged_accepted_lengths_kernel, dim3((unsigned)((a.q.n + 255) / 256)), dim3(256), 0, s, a);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+// Rows of a tile: as in the attention of runs, by the rows of an average sequence,
+// but 16 also where there is so little to do that the shorter way of the few-row
+// kernel counts more than its rate (calls with their merge, us, 16 rows against
+// 128: 128 rows of 256 over 833 keys 16 against 29, 512 rows over 3,000 keys 31
+// against 36, 8 times 32 rows of 128 over 8,192 keys 23 against 31; the other way
+// 8 times 128 rows of 256 over 3,000 keys 47 against 35, 8 times 128 rows of 128
+// over 8,192 keys 49 against 36).  How many workgroups share the batch's work;
+// and the splits that a tile can have at most, which the workspace has room for.
+PagedTreePlan paged_tree_plan(const reflex_paged_cache& c, const reflex_paged_batch& b, int64_t n_rows, int n_q, int dtype) {
+  PagedTreePlan p;
+  const int group = n_q / c.n_kv_heads;
+  const int64_t cap = (int64_t)b.max_pages * c.page_size;
+  const int64_t len = b.max_length > 0 && b.max_length < cap ? b.max_length : cap;
+  p.tile_rows = rows_of_tile(n_rows, b.n_seqs, group, c.n_kv_heads, c.head_dim, dtype);
+  if (dtype == REFLEX_DTYPE_BF16 && n_rows * n_q * c.head_dim <= (1 << 29) / std::max<int64_t>(len, 1)) p.tile_rows = 16;
+#ifdef FORCE_BM
+  p.tile_rows = dtype == REFLEX_DTYPE_BF16 ? FORCE_BM : 16;
+#endif
+  const int64_t slots = p.tile_rows == 128 && c.head_dim > 128 ? 256 : 512;
+  p.units = (int)std::max<int64_t>(1, slots / c.n_kv_heads);
+  const int64_t tiles = (n_rows * group + p.tile_rows - 1) / p.tile_rows;
+  const int64_t row = (int64_t)n_q * (c.head_dim + 2) * sizeof(float) * n_rows;  // bytes of one split of all rows
+  // four times what the tiles would have if they were alike, of 128 keys at least
+  const int64_t most = std::min<int64_t>({64, std::max<int64_t>(1, 4 * p.units / tiles), std::max<int64_t>(1, (len + 127) / 128)});
+  p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(most, (256 << 20) / row));
+  p.bytes = p.nsplit == 1 ? 0 : (size_t)(row * p.nsplit);
+  return p;
 }
 
 template <typename T>

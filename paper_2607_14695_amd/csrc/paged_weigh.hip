@@ -28,14 +28,6 @@ RFX_DEV bool list_of(const PagedAttnArgs& a, int list, List& q) {
   return true;
 }
 
-// r / d for 0 <= r < 2^23, given 1 / d: the product is off by less than one.
-RFX_DEV int divided(int r, int d, float inv) {
-  int q = (int)((float)r * inv);
-  const int rest = r - q * d;
-  q += rest >= d ? 1 : 0;
-  return q - (rest < 0 ? 1 : 0);
-}
-
 // From kept scores: a workgroup sums 4 LANES keys of one list, four of them a lane,
 // and its 256 / LANES groups of lanes take the rows in turn.  64 lanes where rows
 // are few, 16 where they are not: then there are more workgroups, with more rows

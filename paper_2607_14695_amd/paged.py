@@ -281,8 +281,8 @@ class PagedCache:
         tokens before their sequence's rows, and those of these rows that ``mask`` (int64 [rows, words], see
         ``PagedBatch.tree``) names.  Else as ``attend``."""
         m, words = _mask(mask, q.shape[0] if q.dim() else 0, self.device)
-        return self._attend(batch, q, scale, out, "reflex_paged_tree_attention", "reflex_paged_attention_workspace",
-                            m, words)
+        return self._attend(batch, q, scale, out, "reflex_paged_tree_attention",
+                            "reflex_paged_tree_attention_workspace", m, words)
 
     def _attend(self, batch: PagedBatch, q: torch.Tensor, scale: Optional[float], out: Optional[torch.Tensor],
                 call: str, space: str, *args) -> torch.Tensor:

@@ -15,7 +15,7 @@ from paper_2607_14695_amd.paged import PagedBatch, PagedCache, Rotary
 
 from . import draft_reference as ref
 from . import paged_reference as pref
-from .test_gpu_paged import DEV, DT, ROUND, batch, draw, f64, filled, pool
+from .test_gpu_paged import DEV, DT, ROUND, batch, check_attention, draw, f64, filled, pool
 
 pytestmark = pytest.mark.gpu
 
@@ -181,16 +181,19 @@ def test_what_a_drafted_row_does_not_see(new, dtype, store, value):
     np.testing.assert_allclose(got[:bad], before[:bad], atol=moved, rtol=moved)
 
 
-def test_tree_of_a_chain_is_causal_attention():
+@pytest.mark.parametrize("new,dtype", [(3, "bf16"), (100, "bf16"), (30, "f32")])
+def test_tree_of_a_chain_is_causal_attention(new, dtype):
+    """Each within its tolerance of its own definition, of which the two are one and the same here."""
     gen = torch.Generator().manual_seed(4)
-    for new, dtype in ((3, "bf16"), (100, "bf16"), (30, "f32")):
-        cu, lens, table, n_pages = pool([new], [new + 333], 16, gen)
-        cache, _, _ = filled(n_pages, 2, 16, 128, dtype, gen)
-        q = draw(gen, (new, 4, 128), dtype).to(DEV)
-        b = batch(cu, lens, table)
-        mask, pos = b.tree(torch.arange(-1, new - 1, dtype=torch.int32, device=DEV))
-        assert pos.tolist() == list(range(333, 333 + new))
-        assert torch.equal(cache.attend_tree(b, q, mask), cache.attend(b, q))
+    cu, lens, table, n_pages = pool([new], [new + 333], 16, gen)
+    cache, kk, vv = filled(n_pages, 2, 16, 128, dtype, gen)
+    q = draw(gen, (new, 4, 128), dtype)
+    mask, pos = batch(cu, lens, table).tree(torch.arange(-1, new - 1, dtype=torch.int32, device=DEV))
+    assert pos.tolist() == list(range(333, 333 + new))
+    check_tree(q, cache, (kk, vv), cu, lens, table, mask.cpu(), dtype)
+    check_attention(q, cache, (kk, vv), cu, lens, table, True, 0, dtype)
+    seen = ref.in_tree(whole_words(mask), cu.tolist())
+    assert all(list(seen(r, 0, 333 + r, 333 + new)) == list(range(334 + r)) for r in range(new))
 
 
 def test_attend_tree_strides_and_scales():
