@@ -132,6 +132,7 @@ struct PagedAttnArgs {
                      // row splits' sums [row_splits][sequences * K/V heads][score_pitch]
   int64_t score_pitch;
   int row_splits;
+  bool merge_with_sums;  // the splits are joined in the launch that sums the kept scores
 };
 struct PagedAttnPlan {
   int nsplit;
@@ -150,13 +151,15 @@ struct PagedWeighPlan {
   int row_splits;
   int64_t pitch;  // keys that the table holds, or 0
   size_t bytes;   // of the scores or of the splits' sums
+  bool few;       // so few rows that a workgroup sums 256 keys
 };
 PagedWeighPlan paged_weigh_plan(const reflex_paged_cache& c, const reflex_paged_batch& b, int64_t n_rows, int n_q, int dtype);
 template <typename T> hipError_t launch_paged_attention(const PagedAttnArgs& a, int store, hipStream_t s);
 template <typename T> hipError_t launch_paged_tree_attention(const PagedAttnArgs& a, int store, hipStream_t s);
 // keys: the length that the longest sequence is expected to have
 template <typename T>
-hipError_t launch_paged_weighed_attention(const PagedAttnArgs& a, int store, float* weights, int64_t keys, hipStream_t s);
+hipError_t launch_paged_weighed_attention(const PagedAttnArgs& a, int store, float* weights, int64_t keys, bool few,
+                                          hipStream_t s);
 
 constexpr int kMaxTreeWords = 64, kMaxTreeRows = 64 * kMaxTreeWords;
 

@@ -142,6 +142,7 @@ void fill_attention(PagedAttnArgs& a, const reflex_paged_cache* cache, const ref
   a.scores = nullptr;
   a.score_pitch = 0;
   a.row_splits = 1;
+  a.merge_with_sums = false;
 }
 
 int done(hipError_t e) { return e == hipSuccess ? REFLEX_OK : hip_fail(e); }
@@ -362,12 +363,13 @@ int reflex_paged_weighed_attention(const reflex_paged_cache* cache, const reflex
   a.stats = reinterpret_cast<float2*>(stats);
   const PagedWeighPlan p = paged_weigh_plan(*cache, *batch, n_rows, n_q_heads, dtype);
   a.row_splits = p.row_splits;
+  a.merge_with_sums = p.row_splits == 0 && a.nsplit > 1 && p.few;
   a.score_pitch = p.pitch;
   if (p.bytes) a.scores = reinterpret_cast<float*>(stats + whole_256((size_t)n_rows * n_q_heads * sizeof(float2)));
   const int64_t keys = expected_keys(cache, batch);
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  return done(dtype == REFLEX_DTYPE_BF16 ? launch_paged_weighed_attention<bf16_t>(a, cache->store, weights, keys, s)
-                                         : launch_paged_weighed_attention<float>(a, cache->store, weights, keys, s));
+  return done(dtype == REFLEX_DTYPE_BF16 ? launch_paged_weighed_attention<bf16_t>(a, cache->store, weights, keys, p.few, s)
+                                         : launch_paged_weighed_attention<float>(a, cache->store, weights, keys, p.few, s));
 }
 
 int reflex_paged_evict_workspace(const reflex_paged_cache* cache, const reflex_paged_batch* batch, int32_t keep,

@@ -1487,10 +1487,9 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
 // most rows take one memory round trip: 6,144 rows of 256 in five splits 8 us,
 // 32 MB of partial results.
 template <int MODE, typename T, int DH>
-__global__ __launch_bounds__(256) void paged_attn_merge_kernel(const PagedAttnArgs a) {
+RFX_DEV void merge_row(const PagedAttnArgs& a, int64_t id) {
   constexpr int N = DH / 64, G = 8;
   const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int64_t row = id / a.n_q;
   if (row >= a.n_rows) return;
   const float* p = a.part_o + id * a.nsplit * DH + lane * N;
@@ -1537,6 +1536,11 @@ __global__ __launch_bounds__(256) void paged_attn_merge_kernel(const PagedAttnAr
     if (lane == 0) a.stats[id] = make_float2(M, L == 0.f ? 0.f : 1.f / L);
 }
 
+template <int MODE, typename T, int DH>
+__global__ __launch_bounds__(256) void paged_attn_merge_kernel(const PagedAttnArgs a) {
+  merge_row<MODE, T, DH>(a, (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6));
+}
+
 // Tiles that a batch can have at most: every sequence's last one may be partial.
 inline int64_t tile_bound(int64_t n_rows, int n_seqs, int group, int bm) {
   return n_rows * group / bm + std::min<int64_t>(n_seqs, n_rows);
@@ -1577,7 +1581,7 @@ hipError_t launch_shape(const PagedAttnArgs& a, hipStream_t s) {
     if (bm == 32) RFX_LAUNCH((paged_attn_few_kernel<MODE, T, ST, DH, 2>), grid, dim3(256), 0, s, a);
   }
   hipError_t e = hipGetLastError();
-  if (e == hipSuccess && a.nsplit > 1) {
+  if (e == hipSuccess && a.nsplit > 1 && !(MODE == kKept && a.merge_with_sums)) {
     RFX_LAUNCH((paged_attn_merge_kernel<MODE, T, DH>), dim3((unsigned)((a.n_rows * a.n_q + 3) / 4)), dim3(256), 0, s, a);
     e = hipGetLastError();
   }

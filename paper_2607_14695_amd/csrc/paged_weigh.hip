@@ -31,34 +31,81 @@ RFX_DEV bool list_of(const PagedAttnArgs& a, int list, List& q) {
 // From kept scores: a workgroup sums 4 LANES keys of one list, four of them a lane,
 // and its 256 / LANES groups of lanes take the rows in turn.  64 lanes where rows
 // are few, 16 where they are not: then there are more workgroups, with more rows
-// under way in each.
+// under way in each.  With few rows the maxima and sums are joined from the
+// splits' here too, 16 rows at a time under the loads of their scores, so that this need not wait for the merge.
 template <int LANES>
-__global__ __launch_bounds__(256) void paged_weigh_kept_kernel(const PagedAttnArgs a, float* weights, int tiles) {
-  constexpr int KT = 4 * LANES, G = 256 / LANES;
+RFX_DEV void sum_kept(const PagedAttnArgs& a, float* weights, int tiles, int block) {
+  constexpr int KT = 4 * LANES, G = 256 / LANES, SR = 16, PER = SR / G;
   __shared__ float red[G][KT];
-  const int sub = threadIdx.x % LANES, grp = threadIdx.x / LANES;
-  const int list = blockIdx.x / tiles;
+  const int sub = threadIdx.x % LANES, grp = threadIdx.x / LANES, lane = threadIdx.x & 63;
+  const int list = block / tiles;
   List q;
   if (!list_of(a, list, q)) return;
   const float inv_group = 1.f / (float)a.group;
-  for (int64_t t0 = (q.lo & ~(KT - 1)) + (int64_t)(blockIdx.x - list * tiles) * KT; t0 < q.hi; t0 += (int64_t)tiles * KT) {
+  auto id_of = [&](int r, int& tok) __attribute__((always_inline)) {
+    tok = divided(r, a.group, inv_group);
+    return (q.row + tok) * a.n_q + q.kvh * a.group + (r - tok * a.group);
+  };
+  for (int64_t t0 = (q.lo & ~(KT - 1)) + (int64_t)(block - list * tiles) * KT; t0 < q.hi; t0 += (int64_t)tiles * KT) {
     const int key = (int)t0 + 4 * sub;
     const float* const at = a.scores + min((int64_t)key, a.score_pitch - 4);
     // rows of the tokens that see any of these keys
     const int r_lo = (a.causal ? max((int)t0 - q.first, 0) : 0) * a.group;
     const int r_hi = (int)min((int64_t)q.n, a.window > 0 ? t0 + KT - 1 + a.window - q.first : (int64_t)q.n) * a.group;
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int r = r_lo + grp; r < r_hi; r += G) {
-      const int tok = divided(r, a.group, inv_group);
-      const int64_t id = (q.row + tok) * a.n_q + q.kvh * a.group + (r - tok * a.group);
-      const Span sp = span_of(a, q.first + tok, q.len);
-      const float2 st = a.stats[id];
-      const float4 v = *reinterpret_cast<const float4*>(at + id * a.score_pitch);
+    auto load = [&](int r) __attribute__((always_inline)) {
+      int tok;
+      const int64_t id = id_of(r, tok);
+      return *reinterpret_cast<const float4*>(at + id * a.score_pitch);
+    };
+    auto add = [&](int r, const float4& v, const float2& st) __attribute__((always_inline)) {
+      Span sp = span_of(a, q.first + divided(r, a.group, inv_group), q.len);
+      if (r >= r_hi) sp.hi = 0;
       const float x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         acc[i] += key + i >= sp.lo && key + i < sp.hi ? __builtin_amdgcn_exp2f(x[i] - st.x) * st.y : 0.f;
+    };
+    if (LANES == 64 && a.merge_with_sums) {
+      for (int r0 = r_lo; r0 < r_hi; r0 += SR) {
+        // (wave `grp` has rows r0 + 4 u + grp, here and in the sums)
+        float4 v[PER];
+        float2 w[PER];
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+          const int r = min(r0 + G * u + grp, r_hi - 1);
+          int tok;
+          const int64_t id = id_of(r, tok);
+          w[u] = lane < a.nsplit ? a.part_ml[id * a.nsplit + lane] : make_float2(kFloor, 0.f);
+        }
+#pragma unroll
+        for (int u = 0; u < PER; ++u) v[u] = load(min(r0 + G * u + grp, r_hi - 1));
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+          const int r = r0 + G * u + grp;
+          if (r >= r_hi) break;  // (alike in all of the wave)
+          float M = w[u].x;
+#pragma unroll
+          for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+          const float L = warp_sum(w[u].y * __builtin_amdgcn_exp2f(w[u].x - M));
+          add(r, v[u], make_float2(M, L == 0.f ? 0.f : 1.f / L));
+        }
+      }
+    } else {
+      constexpr int U = 4;  // rows of a thread under way
+      for (int r0 = r_lo + grp; r0 < r_hi; r0 += U * G) {
+        float4 v[U];
+        float2 st[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          int tok;
+          const int64_t id = id_of(min(r0 + u * G, r_hi - 1), tok);
+          v[u] = *reinterpret_cast<const float4*>(at + id * a.score_pitch);
+          st[u] = a.stats[id];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) add(r0 + u * G, v[u], st[u]);
+      }
     }
     __syncthreads();  // the last tile's sums have been read
     *reinterpret_cast<float4*>(&red[grp][4 * sub]) = make_float4(acc[0], acc[1], acc[2], acc[3]);
@@ -72,6 +119,20 @@ __global__ __launch_bounds__(256) void paged_weigh_kept_kernel(const PagedAttnAr
       weights[r + ((int64_t)q.kvh << a.c.shift)] += v;
     }
   }
+}
+
+template <int LANES>
+__global__ __launch_bounds__(256) void paged_weigh_kept_kernel(const PagedAttnArgs a, float* weights, int tiles) {
+  sum_kept<LANES>(a, weights, tiles, blockIdx.x);
+}
+
+// The same for few rows, and the merge of their results in the first workgroups:
+// neither waits for the other (64 tokens over 15,409 fp8 keys: 13.5 us together,
+// apart 5 and 10 and the gap between them).
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void paged_weigh_merge_kernel(const PagedAttnArgs a, float* weights, int tiles, int merges) {
+  if ((int)blockIdx.x < merges) merge_row<kPlain, T, DH>(a, (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6));
+  else sum_kept<64>(a, weights, tiles, blockIdx.x - merges);
 }
 
 // Without kept scores: they are formed again.  Each wave holds the fragments of
@@ -395,35 +456,44 @@ PagedWeighPlan paged_weigh_plan(const reflex_paged_cache& c, const reflex_paged_
   const int bm = rows_of_tile(n_rows, b.n_seqs, group, c.n_kv_heads, c.head_dim, dtype);
   const int64_t cap = (int64_t)b.max_pages * c.page_size, pitch = (cap + 63) / 64 * 64;
   const int64_t keys = b.max_length > 0 && b.max_length < cap ? b.max_length : cap;
-  PagedWeighPlan p{0, pitch, (size_t)(pitch * (n_rows * n_q + 1) * 4)};  // (and one that rows of no tile write to)
+  PagedWeighPlan p{0, pitch, (size_t)(pitch * (n_rows * n_q + 1) * 4),  // (and one that rows of no tile write to)
+                   n_rows * group <= 16 * (int64_t)b.n_seqs};
   if (bm <= 32 && p.bytes <= (256 << 20)) return p;
   const int64_t lists = (int64_t)c.n_kv_heads * b.n_seqs;
   const int64_t rows = n_rows * group / std::max<int64_t>(1, std::min<int64_t>(b.n_seqs, n_rows));
   p.row_splits = (int)std::max<int64_t>(1, std::min<int64_t>({4096 / (lists * ((keys + 255) / 256) + 1), rows / 512, 64}));
   p.bytes = (size_t)(lists * p.row_splits * pitch * 4);
-  if (p.row_splits == 1 || p.bytes > (64 << 20)) p = {1, 0, 0};
+  if (p.row_splits == 1 || p.bytes > (64 << 20)) p = {1, 0, 0, false};
   return p;
 }
 
 template <typename T>
-hipError_t launch_paged_weighed_attention(const PagedAttnArgs& a, int store, float* weights, int64_t keys, hipStream_t s) {
+hipError_t launch_paged_weighed_attention(const PagedAttnArgs& a, int store, float* weights, int64_t keys, bool few,
+                                          hipStream_t s) {
   const hipError_t e = a.row_splits ? launch_mode<kWeigh, T>(a, store, s) : launch_mode<kKept, T>(a, store, s);
   if (e != hipSuccess) return e;
   if (a.row_splits == 0) {
     const int64_t lists = (int64_t)a.c.n_kv * a.q.n;
-    const bool few = a.n_rows * a.group <= 16 * (int64_t)a.q.n;
     const int64_t kt = few ? 256 : 64;
     const int64_t tiles = std::min<int64_t>((keys + kt - 1) / kt + 1, std::max<int64_t>(1, (1 << 30) / lists));
-    const dim3 grid((unsigned)(tiles * lists));
-    if (few) RFX_LAUNCH(paged_weigh_kept_kernel<64>, grid, dim3(256), 0, s, a, weights, (int)tiles);
-    else RFX_LAUNCH(paged_weigh_kept_kernel<16>, grid, dim3(256), 0, s, a, weights, (int)tiles);
+    const unsigned grid = (unsigned)(tiles * lists);
+    if (a.merge_with_sums) {
+      const unsigned merges = (unsigned)((a.n_rows * a.n_q + 3) / 4);
+      if (a.c.dh == 64) RFX_LAUNCH((paged_weigh_merge_kernel<T, 64>), dim3(merges + grid), dim3(256), 0, s, a, weights, (int)tiles, (int)merges);
+      else if (a.c.dh == 128) RFX_LAUNCH((paged_weigh_merge_kernel<T, 128>), dim3(merges + grid), dim3(256), 0, s, a, weights, (int)tiles, (int)merges);
+      else RFX_LAUNCH((paged_weigh_merge_kernel<T, 256>), dim3(merges + grid), dim3(256), 0, s, a, weights, (int)tiles, (int)merges);
+    } else if (few) {
+      RFX_LAUNCH(paged_weigh_kept_kernel<64>, dim3(grid), dim3(256), 0, s, a, weights, (int)tiles);
+    } else {
+      RFX_LAUNCH(paged_weigh_kept_kernel<16>, dim3(grid), dim3(256), 0, s, a, weights, (int)tiles);
+    }
     return hipGetLastError();
   }
   if (store == REFLEX_STORE_FP8) return weigh_store<T, REFLEX_STORE_FP8>(a, weights, keys, s);
   if (store == REFLEX_STORE_INT8) return weigh_store<T, REFLEX_STORE_INT8>(a, weights, keys, s);
   return weigh_store<T, REFLEX_STORE_BF16>(a, weights, keys, s);
 }
-template hipError_t launch_paged_weighed_attention<float>(const PagedAttnArgs&, int, float*, int64_t, hipStream_t);
-template hipError_t launch_paged_weighed_attention<bf16_t>(const PagedAttnArgs&, int, float*, int64_t, hipStream_t);
+template hipError_t launch_paged_weighed_attention<float>(const PagedAttnArgs&, int, float*, int64_t, bool, hipStream_t);
+template hipError_t launch_paged_weighed_attention<bf16_t>(const PagedAttnArgs&, int, float*, int64_t, bool, hipStream_t);
 
 }  // namespace reflex

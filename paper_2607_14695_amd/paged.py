@@ -165,11 +165,13 @@ class PagedBatch:
             words = -(-(max_rows if max_rows > 0 else max(n, 1)) // 64)
             if not 1 <= words <= MAX_TREE_WORDS:
                 raise ValueError(f"a tree has at most {64 * MAX_TREE_WORDS} rows a sequence, not {max_rows or n}")
-            out = (torch.empty((n, words), dtype=torch.int64, device=self.device),
-                   torch.empty(n, dtype=torch.int64, device=self.device))
-        mask, positions = out
-        m, words = _mask(mask, n, self.device)
-        pos = _index(positions, (n,), torch.int64, "positions", self.device)
+            mask = torch.empty((n, words), dtype=torch.int64, device=self.device)
+            positions = torch.empty(n, dtype=torch.int64, device=self.device)
+            m, pos = mask.data_ptr(), positions.data_ptr()
+        else:
+            mask, positions = out
+            m, words = _mask(mask, n, self.device)
+            pos = _index(positions, (n,), torch.int64, "positions", self.device)
         _call(self.device, "reflex_paged_tree", load_library().reflex_paged_tree, self._ref, p, n, m, words, pos)
         return mask, positions
 
