@@ -659,7 +659,7 @@ int reflex_paged_attention(const reflex_paged_cache* cache, const reflex_paged_b
  * positions (device int64 [n_rows], may be NULL): lengths[b] - n_b + the number
  * of the row's ancestors, as reflex_paged_write takes them.  A row that the words
  * cannot name sees no row and has the position of one without ancestors.  Rows of
- * no sequence keep what is there.  The page table is not used.
+ * no sequence keep what is there.  The page table is not used.  n_seqs <= 2^18.
  * Errors: REFLEX_EINVAL, REFLEX_EHIP.
  */
 int reflex_paged_tree(const reflex_paged_batch* batch, const int32_t* parents, int64_t n_rows, uint64_t* mask,
@@ -688,7 +688,8 @@ int reflex_paged_tree_attention(const reflex_paged_cache* cache, const reflex_pa
  * what the places behind token c_b hold stays.  If path does not increase, what
  * the accepted tokens hold is undefined.  Pages that rows move in belong to one
  * sequence of the call.  lengths_out may be the batch's lengths; n_b is not cut
- * to a number of rows here.
+ * to a number of rows here.  n_seqs * n_kv_heads <= 2^18, in the two calls below
+ * too.
  * Errors: REFLEX_EINVAL, REFLEX_EHIP.
  */
 int reflex_paged_accept(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const int32_t* path,
@@ -703,7 +704,8 @@ int reflex_paged_accept(const reflex_paged_cache* cache, const reflex_paged_batc
  * order.  A row with zeros as its result adds nothing; one whose scores make its
  * result NaN adds NaN to all that it sees.  Pages whose weights are added to
  * belong to one sequence of the call: where they are shared, additions may be
- * lost.  A page that goes to another sequence needs its weights set to 0.
+ * lost.  A page that goes to another sequence needs its weights set to 0.  The
+ * weights are the call's until its work is done.
  * Errors: as reflex_paged_attention, with a workspace of its own size.
  */
 int reflex_paged_weighed_attention_workspace(const reflex_paged_cache* cache, const reflex_paged_batch* batch,
@@ -727,7 +729,7 @@ int reflex_paged_weighed_attention(const reflex_paged_cache* cache, const reflex
  * cu_rows is not read.  A kept token that is absent reads as zeros, with weight 0.
  * Pages that tokens move in belong to one sequence of the call.  lengths_out may
  * be the batch's lengths.
- * keep: 1 to 2^30, at least sinks + recent; n_seqs * n_kv_heads <= 2^24.
+ * keep: 1 to 2^30, at least sinks + recent.
  * workspace: at least the bytes that reflex_paged_evict_workspace gives,
  * 256-byte aligned; private to the call until its work is done.
  * Errors: REFLEX_EINVAL, REFLEX_EHIP.

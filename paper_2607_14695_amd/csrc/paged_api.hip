@@ -13,6 +13,8 @@ using namespace reflex;
 namespace {
 
 constexpr int64_t kMaxRows = int64_t(1) << 27;
+// sequences times K/V heads where a workgroup, or several, have one of each
+constexpr int64_t kMaxLists = int64_t(1) << 18;
 
 #define RFX_CHECK(expr)              \
   do {                               \
@@ -96,6 +98,10 @@ int elem_bytes(const reflex_paged_cache* c) {
 int64_t expected_keys(const reflex_paged_cache* c, const reflex_paged_batch* b) {
   const int64_t cap = (int64_t)b->max_pages * c->page_size;
   return b->max_length > 0 && b->max_length < cap ? b->max_length : cap;
+}
+
+int check_lists(const reflex_paged_cache* c, const reflex_paged_batch* b) {
+  return (int64_t)b->n_seqs * c->n_kv_heads <= kMaxLists ? REFLEX_OK : REFLEX_EINVAL;
 }
 
 int check_words(int32_t words) { return words >= 1 && words <= kMaxTreeWords ? REFLEX_OK : REFLEX_EINVAL; }
@@ -286,7 +292,7 @@ int reflex_paged_attention(const reflex_paged_cache* cache, const reflex_paged_b
 
 int reflex_paged_tree(const reflex_paged_batch* batch, const int32_t* parents, int64_t n_rows, uint64_t* mask,
                       int32_t mask_words, int64_t* positions, void* stream) {
-  if (!batch || batch->n_seqs < 0 || n_rows < 0 || n_rows > kMaxRows) return REFLEX_EINVAL;
+  if (!batch || batch->n_seqs < 0 || batch->n_seqs > kMaxLists || n_rows < 0 || n_rows > kMaxRows) return REFLEX_EINVAL;
   RFX_CHECK(check_words(mask_words));
   if (n_rows == 0 || batch->n_seqs == 0) return REFLEX_OK;
   if (!batch->cu_rows || !batch->lengths || !parents || !mask || ((uintptr_t)mask & 7) || ((uintptr_t)positions & 7))
@@ -328,6 +334,7 @@ int reflex_paged_accept(const reflex_paged_cache* cache, const reflex_paged_batc
                         int32_t max_path, const int32_t* counts, int32_t* lengths, void* stream) {
   RFX_CHECK(check_cache(cache));
   RFX_CHECK(check_batch(batch, cache, 1));
+  RFX_CHECK(check_lists(cache, batch));
   if (max_path < 0) return REFLEX_EINVAL;
   if (batch->n_seqs == 0) return REFLEX_OK;
   if ((max_path > 0 && !path) || !counts || !lengths) return REFLEX_EINVAL;
@@ -338,6 +345,7 @@ int reflex_paged_accept(const reflex_paged_cache* cache, const reflex_paged_batc
 int reflex_paged_weighed_attention_workspace(const reflex_paged_cache* cache, const reflex_paged_batch* batch,
                                              int64_t n_rows, int32_t n_q_heads, int32_t dtype, size_t* bytes) {
   RFX_CHECK(reflex_paged_attention_workspace(cache, batch, n_rows, n_q_heads, dtype, bytes));
+  RFX_CHECK(check_lists(cache, batch));
   if (n_rows > 0 && batch->n_seqs > 0) {
     const size_t rows = (size_t)n_rows * n_q_heads;
     *bytes = whole_256(whole_256(*bytes) + rows * sizeof(float2)) +
@@ -377,7 +385,8 @@ int reflex_paged_evict_workspace(const reflex_paged_cache* cache, const reflex_p
   if (!bytes) return REFLEX_EINVAL;
   RFX_CHECK(check_cache(cache));
   RFX_CHECK(check_batch(batch, cache, 1));
-  if (keep < 1 || keep > (1 << 30) || (int64_t)batch->n_seqs * cache->n_kv_heads > (1 << 24)) return REFLEX_EINVAL;
+  RFX_CHECK(check_lists(cache, batch));
+  if (keep < 1 || keep > (1 << 30)) return REFLEX_EINVAL;
   *bytes = (size_t)batch->n_seqs * cache->n_kv_heads * (sizeof(int2) + (size_t)keep * sizeof(int32_t));
   return REFLEX_OK;
 }

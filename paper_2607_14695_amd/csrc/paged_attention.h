@@ -373,6 +373,11 @@ RFX_DEV UnitSeq unit_seq(const PagedAttnArgs& a, int b, int bm) {
 }
 RFX_DEV int lanes_sum(int x) { return __builtin_amdgcn_readlane(lanes_up_to(x), 63); }
 RFX_DEV Units count_units(const PagedAttnArgs& a, int bm, int lane, const UnitSeq& first) {
+  if (a.nsplit == 1) {
+    Units u{1 << 30, 0};
+    for (int b0 = 0; b0 < a.q.n; b0 += 64) u.total += lanes_sum((b0 ? unit_seq(a, b0 + lane, bm) : first).tiles);
+    return u;
+  }
   // in units of 128 keys, of which 2^23 rows in tiles of 16 over 2^30 keys make less than 2^43
   int64_t work = 0;
   int longest = 0;

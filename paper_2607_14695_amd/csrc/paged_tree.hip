@@ -181,15 +181,14 @@ PagedTreePlan paged_tree_plan(const reflex_paged_cache& c, const reflex_paged_ba
   const int64_t len = b.max_length > 0 && b.max_length < cap ? b.max_length : cap;
   p.tile_rows = rows_of_tile(n_rows, b.n_seqs, group, c.n_kv_heads, c.head_dim, dtype);
   if (dtype == REFLEX_DTYPE_BF16 && n_rows * n_q * c.head_dim <= (1 << 29) / std::max<int64_t>(len, 1)) p.tile_rows = 16;
-#ifdef FORCE_BM
-  p.tile_rows = dtype == REFLEX_DTYPE_BF16 ? FORCE_BM : 16;
-#endif
   const int64_t slots = p.tile_rows == 128 && c.head_dim > 128 ? 256 : 512;
   p.units = (int)std::max<int64_t>(1, slots / c.n_kv_heads);
   const int64_t tiles = (n_rows * group + p.tile_rows - 1) / p.tile_rows;
   const int64_t row = (int64_t)n_q * (c.head_dim + 2) * sizeof(float) * n_rows;  // bytes of one split of all rows
-  // four times what the tiles would have if they were alike, of 128 keys at least
-  const int64_t most = std::min<int64_t>({64, std::max<int64_t>(1, 4 * p.units / tiles), std::max<int64_t>(1, (len + 127) / 128)});
+  // four times what the tiles would have if they were alike, of 128 keys at least; one
+  // where there are more sequences than CUs, which are tiles enough (and every
+  // workgroup looks all of them over)
+  const int64_t most = b.n_seqs > 256 ? 1 : std::min<int64_t>({64, std::max<int64_t>(1, 4 * p.units / tiles), std::max<int64_t>(1, (len + 127) / 128)});
   p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(most, (256 << 20) / row));
   p.bytes = p.nsplit == 1 ? 0 : (size_t)(row * p.nsplit);
   return p;

@@ -118,8 +118,16 @@ def test_workspaces_are_checked():
     for ws, nb in ((None, size.value), (A, size.value - 1), (A + 128, size.value)):
         assert evict(c, q, keep=100, ws=ws, nb=nb) == R.REFLEX_EINVAL
     assert lib.reflex_paged_evict_workspace(B(c), B(q), 100, None) == R.REFLEX_EINVAL
-    many = batch_c(n_seqs=1 << 24)
+
+
+def test_too_many_sequences_are_refused():
+    c, many = cache_c(), batch_c(n_seqs=(1 << 17) + 1)  # of two heads
+    size = ctypes.c_size_t(0)
+    lib = R.load_library()
     assert lib.reflex_paged_evict_workspace(B(c), B(many), 1, B(size)) == R.REFLEX_EINVAL
+    assert lib.reflex_paged_weighed_attention_workspace(B(c), B(many), 1, 4, 1, B(size)) == R.REFLEX_EINVAL
+    assert evict(batch=many) == accept(batch=many) == weigh(batch=many, n=1) == R.REFLEX_EINVAL
+    assert tree(batch_c(n_seqs=(1 << 18) + 1), n=1) == R.REFLEX_EINVAL
 
 
 def test_python_refusals():

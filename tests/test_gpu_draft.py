@@ -248,6 +248,11 @@ WEIGH = {
     "window": ([(150, 200), (9, 60), (0, 5), (1, 1)], 4, 2, 64, 16, True, 33),
     "window_only": ([(70, 150)], 4, 1, 128, 8, False, 21),
     "before_start": ([(40, 25), (3, 1)], 8, 1, 64, 8, True, 0),
+    # rows of five and three heads, whose tokens end inside the stages, and rows that workgroups divide
+    "heads_of_five": ([(130, 259), (33, 64)], 10, 2, 64, 16, True, 0),
+    "heads_of_three": ([(70, 333), (1, 1)], 3, 1, 256, 32, True, 90),
+    "divided_rows": ([(150, 400)], 8, 1, 128, 16, True, 0),
+    "divided_window": ([(260, 300), (100, 100)], 5, 1, 64, 8, True, 70),
 }
 
 
@@ -261,6 +266,41 @@ def test_weighed(name, dtype, store):
     cu, lens, table, n_pages = pool(news, lengths, ps, gen, more_pages=2)
     cache, kk, vv = filled(n_pages, hk, ps, dh, store, gen)
     check_weighed(draw(gen, (sum(news) + 2, heads, dh), dtype), cache, (kk, vv), cu, lens, table, causal, window, dtype, gen)
+
+
+def test_weighed_strides():
+    """Queries as slices of packed rows, with heads in turn and rows backwards in memory; equal to packed ones."""
+    gen = torch.Generator().manual_seed(31)
+    for new, heads, dtype in ((130, 8, "bf16"), (70, 5, "bf16"), (3, 8, "bf16"), (40, 4, "f32")):
+        cu, lens, table, n_pages = pool([new], [new + 200], 16, gen)
+        cache, _, _ = filled(n_pages, 1, 16, 64, dtype, gen)
+        b = batch(cu, lens, table)
+        packed = torch.randn(new, 3 * heads, 64, generator=gen).to(DT[dtype]).to(DEV)
+        heads_first = packed[:, heads:2 * heads].transpose(0, 1).contiguous().transpose(0, 1)
+        want = cache.zero_weights()
+        cache.attend(b, packed[:, heads:2 * heads].contiguous(), weights=want)
+        for q in (packed[:, heads:2 * heads], heads_first):
+            w = cache.zero_weights()
+            cache.attend(b, q, weights=w)
+            assert torch.equal(w, want)
+
+
+@pytest.mark.parametrize("n_seqs", [70, 300])
+@pytest.mark.parametrize("dtype,store", [("bf16", "bf16"), ("f32", "int8")])
+def test_many_sequences(n_seqs, dtype, store):
+    """More sequences than lanes, and more than CUs; empty ones among them."""
+    gen = torch.Generator().manual_seed(n_seqs)
+    news = [(b * 7) % 5 for b in range(n_seqs)]
+    lengths = [n + (b * 37) % 90 for b, n in enumerate(news)]
+    cu, lens, table, n_pages = pool(news, lengths, 8, gen)
+    cache, kk, vv = filled(n_pages, 1, 8, 64, store, gen)
+    q = draw(gen, (sum(news), 4, 64), dtype)
+    parents = random_parents(news, gen)
+    mask, pos = batch(cu, lens, table).tree(parents.to(DEV), max_rows=4)
+    sees, at = ref.tree(parents.tolist(), cu.tolist(), lengths, 1, sum(news))
+    assert mask[:, 0].tolist() == [ref.words_of(s, 1)[0] for s in sees] and pos.tolist() == at
+    check_tree(q, cache, (kk, vv), cu, lens, table, mask.cpu(), dtype)
+    check_weighed(q, cache, (kk, vv), cu, lens, table, True, 0, dtype, gen)
 
 
 @pytest.mark.parametrize("max_length", [0, 1, 2000])
@@ -445,10 +485,10 @@ def test_accept_many_steps(n, hk, dh, store):
     long_accept(n, hk, dh, store, torch.Generator().manual_seed(n))
 
 
-def check_evict(cache, w, lens, table, keep, sinks, recent):
+def check_evict(cache, w, lens, table, keep, sinks, recent, max_length=0):
     want, ww = raw(cache), w.cpu().numpy().copy()
     kept, new = ref.evict(want, ww, lens.tolist(), table.numpy(), keep, sinks, recent)
-    b = batch(torch.zeros(len(lens) + 1, dtype=torch.int32), lens, table)
+    b = batch(torch.zeros(len(lens) + 1, dtype=torch.int32), lens, table, max_length)
     got = cache.evict(b, w, keep, sinks=sinks, recent=recent)
     np.testing.assert_array_equal(got.cpu().numpy(), kept)
     assert b.tensors[1].tolist() == new
@@ -492,6 +532,17 @@ def test_evict_orders(values):
         w = torch.randint(-2 ** 31, 2 ** 31 - 1, shape, generator=gen).to(torch.int32).view(torch.float32)
     for keep, sinks, recent in ((300, 3, 50), (77, 0, 0)):
         check_evict(cache, w.to(DEV).clone(), lens.clone(), table, keep, sinks, recent)
+
+
+@pytest.mark.parametrize("length", [3000, 4100, 17000])
+def test_evict_longer_than_expected(length):
+    """max_length only sizes the launch."""
+    gen = torch.Generator().manual_seed(length)
+    cu, lens, table, n_pages = pool([0, 0], [length, 77], 16, gen)
+    cache, _, _ = filled(n_pages, 2, 16, 64, "int8", gen)
+    w = torch.round(torch.rand(n_pages, 2, 16, generator=gen) * 999) / 999
+    for keep, max_length in ((length - 5, 100), (1000, 4096)):
+        check_evict(cache, w.to(DEV).clone(), lens.clone(), table, keep, 4, 50, max_length)
 
 
 @pytest.mark.parametrize("length,keep", [(40000, 39000), (70001, 1234), (33000, 32900)])
