@@ -1462,6 +1462,50 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
     seg = seg_end;
   }
 
+  if constexpr (MODE != kPlain) {
+    // Mostly every lane stores its row's dims as it holds them, 16 bytes at a time: a
+    // row at a time by the whole wave, as below, 32 rows took 8 us.
+    auto z = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+    const float l = __uint_as_float(z[0]) + __uint_as_float(z[1]);
+    bool odd = false;
+    if constexpr (ST != REFLEX_STORE_INT8) {
+#pragma unroll
+      for (int d = 0; d < NDB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) odd |= !(fabsf(o[d][i]) < INFINITY);
+    }
+    if (!__syncthreads_or(odd && l < INFINITY && r < t.rows)) {
+      if (r >= t.rows) return;
+      const int64_t row = t.first_row + tok;
+      const int head = kvh * a.group + (r - tok * a.group);
+      if (a.nsplit == 1) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        T* const y = reinterpret_cast<T*>(const_cast<char*>(a.o.p)) + row * a.o.rs + head * a.o.hs + 4 * h;
+#pragma unroll
+        for (int d = 0; d < NDB; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint2*>(y + 32 * d + 8 * i) =
+                make_uint2(pack_bf16(o[d][4 * i] * inv, o[d][4 * i + 1] * inv),
+                           pack_bf16(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv));
+        if (MODE == kWeigh && h == 0) a.stats[row * a.n_q + head] = make_float2(mx, inv);
+        return;
+      }
+      const int64_t at = (row * a.n_q + head) * a.nsplit + split;
+      if (h == 0) a.part_ml[at] = make_float2(mx, l);
+      if (MODE == kTree && split == 0)  // (splits that the tile does not have)
+        for (int s = splits + h; s < a.nsplit; s += 2) a.part_ml[at + s] = make_float2(kFloor, 0.f);
+      if (l == 0.f) return;
+      float* const y = a.part_o + at * DH + 4 * h;
+#pragma unroll
+      for (int d = 0; d < NDB; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<float4*>(y + 32 * d + 8 * i) =
+              make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
+      return;
+    }
+  }
   __syncthreads();
   float* const ex = reinterpret_cast<float*>(smem) + wave * 32 * OP;
   {
