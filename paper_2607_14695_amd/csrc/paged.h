@@ -69,8 +69,8 @@ RFX_DEV int lanes_up_to(int x) {
   return x;
 }
 
-// r / d for 0 <= r <= 2^30 with a quotient below 2^23, given 1 / d: the product is
-// off by less than one.
+// r / d for 0 <= r <= 2^30, given 1 / d rounded (and a quotient below 2^23) or to a
+// unit in the last place (below 2^21): the product is off by less than one.
 RFX_DEV int divided(int r, int d, float inv) {
   int q = (int)((float)r * inv);
   const int rest = r - q * d;

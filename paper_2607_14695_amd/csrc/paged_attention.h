@@ -392,26 +392,30 @@ RFX_DEV Units count_units(const PagedAttnArgs& a, int bm, int lane, const UnitSe
     longest = max(longest, __builtin_amdgcn_readfirstlane(m));
   }
   // keys of a split in 128s, at first
-  int64_t per = max(max((work + a.units - 1) / a.units, (int64_t)((longest + a.nsplit - 1) / a.nsplit)), (int64_t)1);
+  auto rounded_up = [](int64_t x, int d) __attribute__((always_inline)) {
+    if (x < 1 << 22) return (int64_t)divided((int)x + d - 1, d, __builtin_amdgcn_rcpf((float)d));
+    return (x + d - 1) / d;
+  };
+  int64_t per = max(max(rounded_up(work, a.units), rounded_up(longest, a.nsplit)), (int64_t)1);
   Units u;
   // (each tile's last split may be short: once more with what there then are too many)
   for (int turn = 0;; ++turn) {
     u.per = __builtin_amdgcn_readfirstlane((int)min(per * 128, (int64_t)1 << 30));
     u.total = 0;
-    const float inv = 1.f / (float)u.per;
+    const float inv = __builtin_amdgcn_rcpf((float)u.per);
     for (int b0 = 0; b0 < a.q.n; b0 += 64) {
       const UnitSeq s = b0 ? unit_seq(a, b0 + lane, bm) : first;
       u.total += lanes_sum(s.tiles * (s.tiles ? divided(s.keys - 1, u.per, inv) + 1 : 0));
     }
     if (turn == 2 || u.total <= a.units || per >= longest) return u;
-    per = max(per + 1, (per * u.total + a.units - 1) / a.units);
+    per = max(per + 1, rounded_up(per * u.total, a.units));
   }
 }
 // `splits`: how many the tile has; `part`: the unit's keys, of those that any row may see.
 RFX_DEV bool find_unit(const PagedAttnArgs& a, int unit, int bm, int lane, const UnitSeq& first, int per, Tile& t,
                        int& split, int& splits, Span& part) {
   int before = 0;
-  const float inv = 1.f / (float)per;
+  const float inv = __builtin_amdgcn_rcpf((float)per);
   for (int b0 = 0; b0 < a.q.n; b0 += 64) {
     const UnitSeq s = b0 ? unit_seq(a, b0 + lane, bm) : first;
     const int ns = s.tiles ? divided(s.keys - 1, per, inv) + 1 : 0, mine = s.tiles * ns, sum = lanes_up_to(mine);
@@ -420,10 +424,11 @@ RFX_DEV bool find_unit(const PagedAttnArgs& a, int unit, int bm, int lane, const
       const int src = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)past) - 1);
       auto of = [&](int v) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(v, src); };
       const int local = unit - before - (of(sum) - of(mine)), tiles = of(s.tiles);
-      split = __builtin_amdgcn_readfirstlane(local / tiles);
+      split = __builtin_amdgcn_readfirstlane(divided(local, tiles, __builtin_amdgcn_rcpf((float)tiles)));
       splits = of(ns);
       const int keys = of(s.keys);
-      const int alike = __builtin_amdgcn_readfirstlane((keys + 128 * splits - 1) / (128 * splits) * 128);
+      const int alike = __builtin_amdgcn_readfirstlane(
+          (divided(keys - 1, 128 * splits, __builtin_amdgcn_rcpf((float)(128 * splits))) + 1) * 128);
       part.lo = min(split * alike, keys);
       part.hi = min(part.lo + alike, keys);
       t.b = b0 + src;
