@@ -1544,7 +1544,9 @@ template <int MODE, typename T, int DH>
 RFX_DEV void merge_row(const PagedAttnArgs& a, int64_t id) {
   constexpr int N = DH / 64, G = 8;
   const int lane = threadIdx.x & 63;
-  const int64_t row = id / a.n_q;
+  // (there are 2^23 at most: a quotient in 64 bits was most of the instructions)
+  const int64_t row = MODE == kPlain ? id / a.n_q
+                                     : divided((int)id, a.n_q, 1.f / (float)a.n_q);
   if (row >= a.n_rows) return;
   const float* p = a.part_o + id * a.nsplit * DH + lane * N;
   float v[G][N];
@@ -1563,14 +1565,42 @@ RFX_DEV void merge_row(const PagedAttnArgs& a, int64_t id) {
     splits = max(64 - (int)__clzll(__ballot(w.y != 0.f)), 1);
     request(0);
   }
+  float y[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) y[i] = 0.f;
+  auto finish = [&](float M, float L) __attribute__((always_inline)) {
+    store_row<T, DH>(a, row, (int)(id - row * a.n_q), L, y);
+    if constexpr (MODE == kWeigh || MODE == kKept)
+      if (lane == 0) a.stats[id] = make_float2(M, L == 0.f ? 0.f : 1.f / L);
+  };
+  if constexpr (MODE == kTree) {  // (weighed results stay the attention's, bit by bit)
+    if (splits <= G) {
+      // few splits: from lane to lane by scalar reads, which takes a third of the
+      // instructions (28,700 rows of 128 in two splits took 12 us, 94 % vector issue)
+      auto of = [&](float x, int u) __attribute__((always_inline)) {
+        return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), u));
+      };
+      float M = kFloor, L = 0.f;
+#pragma unroll
+      for (int u = 0; u < G; ++u)
+        if (u < splits) M = fmaxf(M, of(w.x, u));
+#pragma unroll
+      for (int u = 0; u < G; ++u)
+        if (u < splits && of(w.y, u) != 0.f) {  // (others have stored no partial sums)
+          const float f = __builtin_amdgcn_exp2f(of(w.x, u) - M);
+          L += of(w.y, u) * f;
+#pragma unroll
+          for (int i = 0; i < N; ++i) y[i] += f * v[u][i];
+        }
+      finish(M, L);
+      return;
+    }
+  }
   float M = w.x;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
   const float f = __builtin_amdgcn_exp2f(w.x - M);
   const float L = warp_sum(w.y * f);
-  float y[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) y[i] = 0.f;
   const uint64_t live = __ballot(w.y != 0.f);  // others have stored no partial sums
   for (int s0 = 0; s0 < a.nsplit; s0 += G) {
     if (s0) {
@@ -1585,9 +1615,7 @@ RFX_DEV void merge_row(const PagedAttnArgs& a, int64_t id) {
         for (int i = 0; i < N; ++i) y[i] += fs * v[u][i];
     }
   }
-  store_row<T, DH>(a, row, (int)(id - row * a.n_q), L, y);
-  if constexpr (MODE == kWeigh || MODE == kKept)
-    if (lane == 0) a.stats[id] = make_float2(M, L == 0.f ? 0.f : 1.f / L);
+  finish(M, L);
 }
 
 template <int MODE, typename T, int DH>

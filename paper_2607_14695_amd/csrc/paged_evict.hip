@@ -31,7 +31,10 @@ constexpr int kTable = 4096;      // table entries held in LDS, if that is all o
 // and writes the chosen ones behind those of the waves before it.
 //
 // A wave has a run of tokens, 64 at a time, the first HELD of these in registers
-// (longer sequences than the launch expected read the others again).
+// with their page rows (longer sequences than the launch expected read the others
+// again).  Vector issue bounds it, 68 % of the cycles of the CUs that it runs on.
+// Places behind the last token have the key 0 as absent tokens do: they come after
+// all others, and there are tokens enough before them.
 template <int HELD>
 __global__ __launch_bounds__(1024) void paged_choose_kernel(const PagedEvictArgs a) {
   __shared__ uint32_t hist[kCopies * kPitch];
@@ -70,24 +73,24 @@ __global__ __launch_bounds__(1024) void paged_choose_kernel(const PagedEvictArgs
   };
   const int chunks = (n + 1023) / 1024, first = wave * chunks * 64 + lane;
   uint32_t key[HELD];
+  int place[HELD];
   {
-    int r[HELD];
     float w[HELD];
 #pragma unroll
-    for (int t = 0; t < HELD; ++t) r[t] = t < chunks ? row_of(lo + min(first + 64 * t, n - 1)) : -1;
+    for (int t = 0; t < HELD; ++t) place[t] = t < chunks ? row_of(lo + min(first + 64 * t, n - 1)) : -1;
 #pragma unroll
-    for (int t = 0; t < HELD; ++t) w[t] = a.weights[max(r[t], 0)];
+    for (int t = 0; t < HELD; ++t) w[t] = a.weights[max(place[t], 0)];
 #pragma unroll
-    for (int t = 0; t < HELD; ++t) key[t] = r[t] < 0 ? 0u : order_of(w[t]);
+    for (int t = 0; t < HELD; ++t) key[t] = place[t] < 0 || first + 64 * t >= n ? 0u : order_of(w[t]);
   }
-  // f(token, key) of the run's tokens; all of the wave's lanes come to it
+  // f(token, page row, key) of the run's places; all of the wave's lanes come to it
   auto each = [&](auto f) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < HELD; ++t)
-      if (t < chunks) f(first + 64 * t, key[t]);
+      if (t < chunks) f(first + 64 * t, place[t], key[t]);
     for (int t = HELD; t < chunks; ++t) {
-      const int j = first + 64 * t, r = row_of(lo + min(j, n - 1));
-      f(j, r < 0 ? 0u : order_of(a.weights[r]));
+      const int j = first + 64 * t, r = j < n ? row_of(lo + j) : -1;
+      f(j, r, r < 0 ? 0u : order_of(a.weights[r]));
     }
   };
   // sum of the waves before this one
@@ -104,12 +107,10 @@ __global__ __launch_bounds__(1024) void paged_choose_kernel(const PagedEvictArgs
   for (int pass = 0; pass < 3 && need > 0; ++pass) {
     const int at = pass == 0 ? 21 : pass == 1 ? 10 : 0, last = pass == 2 ? 1023 : 2047;
     if (pass == 0)
-      each([&](int j, uint32_t k) __attribute__((always_inline)) {
-        if (j < n) atomicAdd(&bins[k >> 21], 1u);
-      });
+      each([&](int, int, uint32_t k) __attribute__((always_inline)) { atomicAdd(&bins[k >> 21], 1u); });
     else
-      each([&](int j, uint32_t k) __attribute__((always_inline)) {
-        if (j < n && k >> (pass == 1 ? 21 : 10) == top) atomicAdd(&bins[(k >> at) & last], 1u);
+      each([&](int, int, uint32_t k) __attribute__((always_inline)) {
+        if (k >> (pass == 1 ? 21 : 10) == top) atomicAdd(&bins[(k >> at) & last], 1u);
       });
     __syncthreads();
     // thread t has bins 2 t', 2 t' + 1 with t' counted from the top; it leaves zeros
@@ -145,11 +146,9 @@ __global__ __launch_bounds__(1024) void paged_choose_kernel(const PagedEvictArgs
   }
 
   int more = 0, same = 0;
-  each([&](int j, uint32_t k) __attribute__((always_inline)) {
-    if (j < n) {
-      more += k > top;
-      same += k == top;
-    }
+  each([&](int, int, uint32_t k) __attribute__((always_inline)) {
+    more += k > top;
+    same += k == top;
   });
   more = lanes_up_to(more);
   same = lanes_up_to(same);
@@ -162,20 +161,20 @@ __global__ __launch_bounds__(1024) void paged_choose_kernel(const PagedEvictArgs
   more = before_wave(part);
   same = before_wave(part_eq);
   const uint64_t below = (1ull << lane) - 1;
-  auto put = [&](int i, int j) __attribute__((always_inline)) {
-    from[i] = row_of(j);
+  auto put = [&](int i, int j, int r) __attribute__((always_inline)) {
+    from[i] = r;
     if (kept) kept[i] = j;
   };
-  each([&](int j, uint32_t k) __attribute__((always_inline)) {
-    const uint64_t gt = __ballot(j < n && k > top), eq = __ballot(j < n && k == top);
+  each([&](int j, int r, uint32_t k) __attribute__((always_inline)) {
+    const uint64_t gt = __ballot(k > top), eq = __ballot(k == top);
     const int eq_before = same + __popcll(eq & below);
-    if (j < n && (k > top || (k == top && eq_before < left)))
-      put(lo + more + __popcll(gt & below) + min(eq_before, left), lo + j);
+    if (k > top || (k == top && eq_before < left))
+      put(lo + more + __popcll(gt & below) + min(eq_before, left), lo + j, r);
     more += __popcll(gt);
     same += __popcll(eq);
   });
-  for (int i = tid; i < a.sinks; i += 1024) put(i, i);
-  for (int i = tid; i < a.recent; i += 1024) put(a.keep - a.recent + i, hi + i);
+  for (int i = tid; i < a.sinks; i += 1024) put(i, i, row_of(i));
+  for (int i = tid; i < a.recent; i += 1024) put(a.keep - a.recent + i, hi + i, row_of(hi + i));
 }
 
 // Token i of a list from page row from[i], in order: from[i] is that of a token

@@ -133,7 +133,7 @@ __global__ __launch_bounds__(256) void paged_weigh_kept_kernel(const PagedAttnAr
 // apart 5 and 10 and the gap between them).
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void paged_weigh_merge_kernel(const PagedAttnArgs a, float* weights, int tiles, int merges) {
-  if ((int)blockIdx.x < merges) merge_row<kPlain, T, DH>(a, (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6));
+  if ((int)blockIdx.x < merges) merge_row<kKept, T, DH>(a, (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6));
   else sum_kept<64>(a, weights, tiles, blockIdx.x - merges);
 }
 
