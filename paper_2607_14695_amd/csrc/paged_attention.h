@@ -352,8 +352,9 @@ RFX_DEV int count_tiles(const PagedAttnArgs& a, int bm, int lane) {
 // kTree: trees are small, and the sequences below them differ in length, so tiles
 // are not split alike: the batch's work (tiles x keys) is divided by the number of
 // workgroups that the chip holds, and every tile has as many splits, alike ones, as
-// that many keys to a split ask for.  32 ragged trees of 26 to 64 rows of 8 heads over 3,000 to
-// 15,409 fp8 keys took 327 us with two splits each (the longest ones' time).
+// that many keys to a split ask for.  32 ragged trees of 26 to 64 rows of 8 heads
+// of 256 over 3,344 to 15,409 fp8 keys take 242 us (505 TFLOP/s); with two splits
+// each they took 327, the longest ones' time.
 //
 // A unit is a tile's split; units are numbered over the sequences, in each over
 // the splits and in these over the tiles, which share the split's keys.
@@ -1469,7 +1470,8 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void paged_attn_many_kernel
 
   if constexpr (MODE != kPlain) {
     // Mostly every lane stores its row's dims as it holds them, 16 bytes at a time: a
-    // row at a time by the whole wave, as below, 32 rows took 8 us.
+    // row at a time by the whole wave, as below, 32 rows take 8 us (8 trees of 64
+    // rows of 32 heads over 8,192 keys 96 us that way, 87 this way).
     auto z = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
     const float l = __uint_as_float(z[0]) + __uint_as_float(z[1]);
     bool odd = false;
