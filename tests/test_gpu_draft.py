@@ -248,6 +248,7 @@ WEIGH = {
     "window": ([(150, 200), (9, 60), (0, 5), (1, 1)], 4, 2, 64, 16, True, 33),
     "window_only": ([(70, 150)], 4, 1, 128, 8, False, 21),
     "before_start": ([(40, 25), (3, 1)], 8, 1, 64, 8, True, 0),
+    "widest_window": ([(40, 60), (1, 33)], 4, 1, 64, 8, False, 2 ** 31 - 1),
     # rows of five and three heads, whose tokens end inside the stages, and rows that workgroups divide
     "heads_of_five": ([(130, 259), (33, 64)], 10, 2, 64, 16, True, 0),
     "heads_of_three": ([(70, 333), (1, 1)], 3, 1, 256, 32, True, 90),
@@ -778,3 +779,64 @@ def test_drafting_over_a_bounded_memory():
         for g in range(hk):
             model[s][g].append([rk[s, g], f64(v)[s, g], -1, 0.0])
         np.testing.assert_allclose(got[s], attended(s, rq[s], lambda j: True), atol=2e-5)
+
+
+def test_pages_past_4_gib():
+    """The same sequences in the last pages of a cache of 4.6 GB a side: the same bits as in a small one."""
+    gen = torch.Generator().manual_seed(17)
+    news, lengths, ps, dh, far = [1, 12, 40], [300, 200, 333], 64, 256, 70000
+    cu, lens, table, n_pages = pool(news, lengths, ps, gen)
+    small, _, _ = filled(n_pages, 1, ps, dh, "f32", gen)
+    big = PagedCache.zeros(far + n_pages, ps, 1, dh, torch.float32)
+    big.k[far:], big.v[far:] = small.k, small.v
+    assert big.k[far].data_ptr() - big.k.data_ptr() > 2 ** 32
+    q = draw(gen, (sum(news), 4, dh), "f32").to(DEV)
+    mask = torch.randint(-2 ** 63, 2 ** 63 - 1, (sum(news), 1), generator=gen).to(DEV)
+    path, counts = torch.tensor([[0, 0], [3, 9], [0, 38]], dtype=torch.int32, device=DEV), torch.tensor(
+        [1, 2, 2], dtype=torch.int32, device=DEV)
+    got = []
+    for cache, shift in ((small, 0), (big, far)):
+        b = batch(cu, lens, torch.where(table >= 0, table + shift, table))
+        w = cache.zero_weights()
+        outs = [cache.attend_tree(b, q, mask), cache.attend(b, q, weights=w), w[shift:].clone()]
+        cache.accept(b, path, counts)
+        outs += [cache.evict(b, w, 150, sinks=3, recent=20), w[shift:], b.tensors[1], cache.k[shift:], cache.v[shift:]]
+        assert not shift or not (w[:shift].any() or cache.k[:shift].any() or cache.v[:shift].any())
+        got.append(outs)
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
+
+
+def test_c_entries_without_what_is_optional():
+    """No positions, no list of kept tokens, lengths written to an array of their own."""
+    import ctypes
+    gen = torch.Generator().manual_seed(19)
+    cu, lens, table, n_pages = pool([5, 9], [60, 90], 8, gen)
+    lib, ref_ = R.load_library(), ctypes.byref
+    one, two = (filled(n_pages, 2, 8, 64, "int8", torch.Generator().manual_seed(3))[0] for _ in range(2))
+    b1, b2 = batch(cu, lens, table), batch(cu, lens, table)
+    s = torch.cuda.current_stream().cuda_stream
+    parents = random_parents([5, 9], gen).to(DEV)
+    mask, _ = b1.tree(parents, max_rows=9)
+    mask2 = torch.zeros_like(mask)
+    assert lib.reflex_paged_tree(ref_(b2.c), parents.data_ptr(), 14, mask2.data_ptr(), 1, None, s) == R.REFLEX_OK
+    assert torch.equal(mask, mask2)
+    path = torch.tensor([[0, 2, 4], [1, 3, 8]], dtype=torch.int32, device=DEV)
+    counts = torch.tensor([2, 3], dtype=torch.int32, device=DEV)
+    one.accept(b1, path, counts)
+    other = torch.zeros(2, dtype=torch.int32, device=DEV)
+    assert lib.reflex_paged_accept(ref_(two.c), ref_(b2.c), path.data_ptr(), 3, counts.data_ptr(), other.data_ptr(),
+                                   s) == R.REFLEX_OK
+    assert b2.tensors[1].tolist() == [60, 90] and torch.equal(other, b1.tensors[1])
+    same_pages(two, raw(one))
+    b3 = batch(cu, other.cpu(), table)
+    w1 = torch.rand(n_pages, 2, 8, generator=gen).to(DEV)
+    w2 = w1.clone()
+    one.evict(b1, w1, 33, sinks=1, recent=7)
+    ws = torch.empty(2 * 2 * (8 + 33 * 4), dtype=torch.uint8, device=DEV)
+    out = torch.zeros(2, dtype=torch.int32, device=DEV)
+    assert lib.reflex_paged_evict(ref_(two.c), ref_(b3.c), w2.data_ptr(), 33, 1, 7, None, out.data_ptr(), ws.data_ptr(),
+                                  ws.numel(), s) == R.REFLEX_OK
+    assert torch.equal(w1, w2) and out.tolist() == b1.tensors[1].tolist() == [33, 33]
+    assert b3.tensors[1].tolist() == other.tolist()
+    same_pages(two, raw(one))
