@@ -973,23 +973,56 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
   }
   __syncthreads();
   constexpr int N = DH / 64;
-  for (int q = wave; q < rows_here; q += 4) {
-    float M = kFloor;
+  if constexpr (MODE == kTree) {
+    // (Four rows' reads at once: a tree of 16 rows of 8 heads of 256 over 833 keys 11.5
+    // instead of 12.6 us; single weighed tokens, which have one or two rows a wave, no less.)
+    for (int q0 = wave; q0 < rows_here; q0 += 16) {
+      float M[4], L[4], y[4][N];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) M = fmaxf(M, ml[w][q].x);
-    float L = 0.f, y[N];
+      for (int u = 0; u < 4; ++u) {
+        const int q = q0 + 4 * u;
+        M[u] = kFloor;
 #pragma unroll
-    for (int i = 0; i < N; ++i) y[i] = 0.f;
+        for (int w = 0; w < 4; ++w) M[u] = fmaxf(M[u], ml[w][q].x);
+        L[u] = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float f = __builtin_amdgcn_exp2f(ml[w][q].x - M);
-      L += ml[w][q].y * f;
+        for (int i = 0; i < N; ++i) y[u][i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < N; ++i) y[i] += f * ex[(w * BM + q) * OP + lane * N + i];
+        for (int w = 0; w < 4; ++w) {
+          const float f = __builtin_amdgcn_exp2f(ml[w][q].x - M[u]);
+          L[u] += ml[w][q].y * f;
+#pragma unroll
+          for (int i = 0; i < N; ++i) y[u][i] += f * ex[(w * BM + q) * OP + lane * N + i];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int q = q0 + 4 * u;
+        if (q >= rows_here) break;
+        const int r = t.r0 + q, tok = r / a.group, head = kvh * a.group + (r - tok * a.group);
+        const int64_t row = t.first_row + tok;
+        finish_row<MODE, T, ST, DH>(a, blockIdx.x, BM, q, row, head, split, BF, M[u], L[u], y[u], splits);
+      }
     }
-    const int r = t.r0 + q, tok = r / a.group, head = kvh * a.group + (r - tok * a.group);
-    const int64_t row = t.first_row + tok;
-    finish_row<MODE, T, ST, DH>(a, blockIdx.x, BM, q, row, head, split, BF, M, L, y, splits);
+  } else {
+    for (int q = wave; q < rows_here; q += 4) {
+      float M = kFloor;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) M = fmaxf(M, ml[w][q].x);
+      float L = 0.f, y[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) y[i] = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(ml[w][q].x - M);
+        L += ml[w][q].y * f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] += f * ex[(w * BM + q) * OP + lane * N + i];
+      }
+      const int r = t.r0 + q, tok = r / a.group, head = kvh * a.group + (r - tok * a.group);
+      const int64_t row = t.first_row + tok;
+      finish_row<MODE, T, ST, DH>(a, blockIdx.x, BM, q, row, head, split, BF, M, L, y, splits);
+    }
   }
 }
 
