@@ -1598,7 +1598,7 @@ RFX_DEV void merge_row(const PagedAttnArgs& a, int64_t id) {
   if (row < a.q.cu[0] || row >= a.q.cu[a.q.n]) return;
   if constexpr (MODE == kTree) {  // a tile may have few of the splits that there is room for
     splits = max(64 - (int)__clzll(__ballot(w.y != 0.f)), 1);
-    request(0);
+    if (splits <= G) request(0);
   }
   float y[N];
 #pragma unroll
@@ -1637,6 +1637,39 @@ RFX_DEV void merge_row(const PagedAttnArgs& a, int64_t id) {
   const float f = __builtin_amdgcn_exp2f(w.x - M);
   const float L = warp_sum(w.y * f);
   const uint64_t live = __ballot(w.y != 0.f);  // others have stored no partial sums
+  if constexpr (MODE == kTree) {
+    // Many splits: four are added and asked for anew while four are under way.  For one
+    // that is not live the last one, which is, is read, without a branch, and not added
+    // (64 rows of 8 heads of 256 in 64 splits 7.6 instead of 14.0 us, eight at a time).
+    auto fetch = [&](int u0, int s0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < G / 2; ++u) {
+        const int s = s0 + u < splits && ((live >> ((s0 + u) & 63)) & 1) ? s0 + u : splits - 1;
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[u0 + u][i] = p[s * DH + i];
+      }
+    };
+    auto add = [&](int u0, int s0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < G / 2; ++u) {
+        const int s = s0 + u;
+        if (s >= splits || !((live >> s) & 1)) continue;
+        const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s));
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] += fs * v[u0 + u][i];
+      }
+    };
+    fetch(0, 0);
+    fetch(G / 2, G / 2);
+    for (int s0 = 0; s0 < splits; s0 += G) {
+      add(0, s0);
+      fetch(0, s0 + G);
+      add(G / 2, s0 + G / 2);
+      fetch(G / 2, s0 + G + G / 2);
+    }
+    finish(M, L);
+    return;
+  }
   for (int s0 = 0; s0 < a.nsplit; s0 += G) {
     if (s0) {
       if (!(live >> s0)) break;

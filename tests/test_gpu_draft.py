@@ -181,6 +181,28 @@ def test_what_a_drafted_row_does_not_see(new, dtype, store, value):
     np.testing.assert_allclose(got[:bad], before[:bad], atol=moved, rtol=moved)
 
 
+@pytest.mark.parametrize("new,dtype", [(2, "bf16"), (64, "bf16"), (12, "f32")])
+@pytest.mark.parametrize("token", [3, 5000, 8190])
+def test_an_infinite_value_over_many_splits(new, dtype, token):
+    """An infinite element of a value that all rows see is theirs in that dim, in whichever of the splits it lies and
+    whichever of them have no token; the other dims are as without it."""
+    gen = torch.Generator().manual_seed(new)
+    cu, lens, table, n_pages = pool([new], [new + 8191], 16, gen)
+    table[0, 100:250] = -1  # (whole splits of absent tokens)
+    cache, kk, vv = filled(n_pages, 1, 16, 128, dtype, gen)
+    mask = batch(cu, lens, table).tree(random_parents([new], gen).to(DEV))[0].cpu()
+    q = draw(gen, (new, 4, 128), dtype)
+    before = check_tree(q, cache, (kk, vv), cu, lens, table, mask, dtype)
+    page, slot = pref.place(table[0], n_pages, 16, token)
+    cache.v[page, 0, slot, 7] = float("inf")
+    got = f64(cache.attend_tree(batch(cu, lens, table), q.to(DEV), mask.to(DEV)))
+    assert np.all(got[..., 7] == np.inf)
+    # (a row that is taken again key by key is rounded otherwise)
+    others = np.arange(128) != 7
+    moved = 2.0 ** -6 if dtype == "bf16" else 1e-5
+    np.testing.assert_allclose(got[..., others], before[..., others], atol=moved, rtol=moved)
+
+
 @pytest.mark.parametrize("new,dtype", [(3, "bf16"), (100, "bf16"), (30, "f32")])
 def test_tree_of_a_chain_is_causal_attention(new, dtype):
     """Each within its tolerance of its own definition, of which the two are one and the same here."""
