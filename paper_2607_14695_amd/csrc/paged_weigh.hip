@@ -458,7 +458,8 @@ hipError_t weigh_store(const PagedAttnArgs& a, float* weights, int64_t keys, hip
 // for a workspace that is hardly used.
 //
 // Else the rows of a list are divided where lists and tiles of 256 keys alone
-// would not make sixteen workgroups for every CU, with 512 rows at least to each.
+// would not make sixteen workgroups for every CU, with 512 rows at least to each
+// (and not over a table of no pages, which leaves no sums to join).
 PagedWeighPlan paged_weigh_plan(const reflex_paged_cache& c, const reflex_paged_batch& b, int64_t n_rows, int n_q, int dtype) {
   const int group = n_q / c.n_kv_heads;
   const int bm = rows_of_tile(n_rows, b.n_seqs, group, c.n_kv_heads, c.head_dim, dtype);
@@ -471,7 +472,7 @@ PagedWeighPlan paged_weigh_plan(const reflex_paged_cache& c, const reflex_paged_
   const int64_t rows = n_rows * group / std::max<int64_t>(1, std::min<int64_t>(b.n_seqs, n_rows));
   p.row_splits = (int)std::max<int64_t>(1, std::min<int64_t>({4096 / (lists * ((keys + 255) / 256) + 1), rows / 512, 64}));
   p.bytes = (size_t)(lists * p.row_splits * pitch * 4);
-  if (p.row_splits == 1 || p.bytes > (64 << 20)) p = {1, 0, 0, false};
+  if (p.row_splits == 1 || p.bytes == 0 || p.bytes > (64 << 20)) p = {1, 0, 0, false};
   return p;
 }
 
