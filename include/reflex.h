@@ -684,12 +684,12 @@ int reflex_paged_tree_attention(const reflex_paged_cache* cache, const reflex_pa
  * becomes lengths[b] - n_b + c_b (at least 0).  path: device int32
  * [n_seqs][max_path], strictly increasing up to c_b, as the rows of a way down a
  * tree are; counts: device int32 [n_seqs], c_b = counts[b] cut to [0, min(n_b,
- * max_path)].  A row outside [0, n_b), or whose token is absent, reads as zeros;
- * what the places behind token c_b hold stays.  If path does not increase, what
- * the accepted tokens hold is undefined.  Pages that rows move in belong to one
- * sequence of the call.  lengths_out may be the batch's lengths; n_b is not cut
- * to a number of rows here.  n_seqs * n_kv_heads <= 2^18, in the two calls below
- * too.
+ * max_path)].  A row outside [0, n_b), a negative one among them, or whose token
+ * is absent, reads as zeros; what the places behind token c_b hold stays.  If
+ * path does not increase, what the accepted tokens hold is undefined.  Pages that
+ * rows move in belong to one sequence of the call.  lengths_out may be the batch's
+ * lengths; n_b is not cut to a number of rows here.  n_seqs * n_kv_heads <= 2^18,
+ * in the two calls below too.
  * Errors: REFLEX_EINVAL, REFLEX_EHIP.
  */
 int reflex_paged_accept(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const int32_t* path,

@@ -52,14 +52,17 @@ __global__ __launch_bounds__(256) void paged_tree_kernel(const PagedTreeArgs a) 
 }
 
 // Accepted rows of a sequence moved to its end: token first + i from token first
-// + path[i].  Both go up and path[i] >= i, so a place is never read after a
-// later step has written it: the workgroup takes the moves in order, some
-// thousands of bytes a step, and stores a step only when all of it was read.
-// One workgroup to a sequence, which also writes its length (32 sequences of 6
-// tokens of one 256-wide head 3.7 us, a chain of latencies); where that would be
-// many bytes, one to each `per_part` heads, and the lengths in a launch of their
-// own (8 sequences of up to 90 tokens of 8 heads of 128 took 31 us in 8
-// workgroups).
+// + path[i].  The path goes up, so path[i] - i never falls: tokens that come from
+// a lower place (none, unless the path begins with negative entries, which read as
+// zeros) are the first `up` ones, and these come from places among their own.  They
+// are taken from the last to the first, the others, with path[i] >= i, from the
+// first to the last: either way a place is never read after a later step has
+// written it.  A step is some thousands of bytes, and is stored only when all of it
+// was read.  One workgroup to a sequence, which also writes its length (32
+// sequences of 6 tokens of one 256-wide head 3.7 us, a chain of latencies); where
+// that would be many bytes, one to each `per_part` heads, and the lengths in a
+// launch of their own (8 sequences of up to 90 tokens of 8 heads of 128 took 31 us
+// in 8 workgroups).
 struct Accepted { int64_t n, first; int c; };
 RFX_DEV Accepted accepted_of(const PagedAcceptArgs& a, int b) {
   Accepted x;
@@ -69,69 +72,89 @@ RFX_DEV Accepted accepted_of(const PagedAcceptArgs& a, int b) {
   return x;
 }
 
+// How many of the accepted tokens come from a lower place than theirs.
+RFX_DEV int from_below(const int32_t* path, int p0, int c) {
+  if (c == 0 || p0 >= 0) return 0;
+  int lo = 1, hi = c;
+  while (lo < hi) {
+    const int i = (lo + hi) >> 1;
+    if (path[i] < i) lo = i + 1;
+    else hi = i;
+  }
+  return lo;
+}
+
+// The moves of c tokens of `per` values each, U values of a thread a step; place(i,
+// w, to, from) finds value w of token i: nowhere if `to` is left, zero if `from` is.
+template <typename V, int U, typename F>
+RFX_DEV void move_accepted(int c, int up, int per, F place) {
+  auto step = [&](int64_t e0, int64_t end) __attribute__((always_inline)) {
+    V v[U];
+    V* to[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t e = e0 + u * 1024 + threadIdx.x;
+      to[u] = nullptr;
+      v[u] = V{};
+      if (e >= end) continue;
+      const int i = (int)(e / per);
+      const V* from = nullptr;
+      place(i, (int)(e - (int64_t)i * per), to[u], from);
+      if (from) v[u] = *from;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if constexpr (sizeof(V) == 16) asm volatile("" : "+v"(v[u].x), "+v"(v[u].y), "+v"(v[u].z), "+v"(v[u].w));
+      else asm volatile("" : "+v"(v[u]));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (to[u]) *to[u] = v[u];
+  };
+  constexpr int kStep = 1024 * U;
+  const int64_t below = (int64_t)up * per, all = (int64_t)c * per;
+  for (int64_t e0 = (below - 1) / kStep * kStep; below > 0 && e0 >= 0; e0 -= kStep) step(e0, below);
+  for (int64_t e0 = below; e0 < all; e0 += kStep) step(e0, all);
+}
+
 constexpr int kAcceptUnits = 4;  // 16-byte pieces of a thread and step
 __global__ __launch_bounds__(1024) void paged_accept_kernel(const PagedAcceptArgs a, int row_bytes, int scaled, int per_part) {
   const int parts = (a.c.n_kv + per_part - 1) / per_part;
   const int b = blockIdx.x / parts, h0 = (blockIdx.x - b * parts) * per_part, heads = min(per_part, a.c.n_kv - h0);
-  const Accepted x = accepted_of(a, b);
   const int32_t* const path = a.path + (int64_t)b * a.max_path;
+  const int p0 = a.max_path > 0 ? path[0] : 0;  // (under way with the lengths)
+  const Accepted x = accepted_of(a, b);
+  const int up = from_below(path, p0, x.c);
   // (page row of head 0 that accepted token i comes from, and goes to)
   auto places = [&](int i, int& src, int& dst) __attribute__((always_inline)) {
     const int p = path[i];
     dst = page_row(a.c, a.q, b, x.first + i);
     src = p < 0 || p >= x.n ? -1 : page_row(a.c, a.q, b, x.first + p);
   };
-  const int per_row = row_bytes / 16;
-  const int units = 2 * heads * per_row;  // of a token: K and V of the heads
-  const int64_t all = (int64_t)x.c * units;
-  for (int64_t e0 = 0; e0 < all; e0 += 1024 * kAcceptUnits) {
-    uint4 v[kAcceptUnits];
-    char* to[kAcceptUnits];
-#pragma unroll
-    for (int u = 0; u < kAcceptUnits; ++u) {
-      const int64_t e = e0 + u * 1024 + threadIdx.x;
-      to[u] = nullptr;
-      v[u] = zero16();
-      if (e >= all) continue;
-      const int i = (int)(e / units), w = (int)(e - (int64_t)i * units);
-      const int side = w / (units / 2), y = w - side * (units / 2);
-      const int h = y / per_row, piece = y - h * per_row;
+  const int per_row = row_bytes / 16, side_units = heads * per_row;  // of a token: K and V of the heads
+  move_accepted<uint4, kAcceptUnits>(x.c, up, 2 * side_units, [&](int i, int w, uint4*& to, const uint4*& from)
+                                     __attribute__((always_inline)) {
+    const int side = w / side_units, y = w - side * side_units;
+    const int h = y / per_row, piece = y - h * per_row;
+    int src, dst;
+    places(i, src, dst);
+    if (dst < 0 || src == dst) return;
+    char* const base = side ? a.c.v : a.c.k;
+    const int64_t hoff = (int64_t)(h0 + h) << a.c.shift;
+    to = reinterpret_cast<uint4*>(base + (dst + hoff) * row_bytes + piece * 16);
+    if (src >= 0) from = reinterpret_cast<const uint4*>(base + (src + hoff) * row_bytes + piece * 16);
+  });
+  if (scaled) {
+    move_accepted<float, 1>(x.c, up, 2 * heads, [&](int i, int w, float*& to, const float*& from)
+                            __attribute__((always_inline)) {
       int src, dst;
       places(i, src, dst);
-      if (dst < 0 || src == dst) continue;
-      char* const base = side ? a.c.v : a.c.k;
-      const int64_t hoff = (int64_t)(h0 + h) << a.c.shift;
-      to[u] = base + (dst + hoff) * row_bytes + piece * 16;
-      if (src >= 0) v[u] = ld16(base + (src + hoff) * row_bytes + piece * 16);
-    }
-#pragma unroll
-    for (int u = 0; u < kAcceptUnits; ++u) asm volatile("" : "+v"(v[u].x), "+v"(v[u].y), "+v"(v[u].z), "+v"(v[u].w));
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < kAcceptUnits; ++u)
-      if (to[u]) st16(to[u], v[u]);
-  }
-  if (scaled) {
-    const int per = 2 * heads;
-    const int64_t total = (int64_t)x.c * per;
-    for (int64_t e0 = 0; e0 < total; e0 += 1024) {
-      const int64_t e = e0 + threadIdx.x;
-      float v = 0.f;
-      float* to = nullptr;
-      if (e < total) {
-        const int i = (int)(e / per), w = (int)(e - (int64_t)i * per);
-        int src, dst;
-        places(i, src, dst);
-        if (dst >= 0 && src != dst) {
-          float* const base = (w >= heads ? a.c.v_scale : a.c.k_scale) + ((int64_t)(h0 + w % heads) << a.c.shift);
-          to = base + dst;
-          if (src >= 0) v = base[src];
-        }
-      }
-      asm volatile("" : "+v"(v));
-      __syncthreads();
-      if (to) *to = v;
-    }
+      if (dst < 0 || src == dst) return;
+      float* const base = (w >= heads ? a.c.v_scale : a.c.k_scale) + ((int64_t)(h0 + w % heads) << a.c.shift);
+      to = base + dst;
+      if (src >= 0) from = base + src;
+    });
   }
   if (parts > 1) return;
   __syncthreads();  // every thread has read the length

@@ -1,11 +1,12 @@
 """GPU checks of drafted tokens and a bounded memory where a call meets the edge of what its arguments allow: tables
-without pages, lengths past the table."""
+without pages, lengths past the table, paths below the rows."""
 import numpy as np
 import pytest
 import torch
 
 from paper_2607_14695_amd.paged import PagedBatch
 
+from . import draft_reference as ref
 from .test_gpu_draft import raw, same_pages
 from .test_gpu_paged import DEV, batch, draw, filled, pool
 
@@ -47,3 +48,32 @@ def test_a_table_of_no_pages(news, heads, dtype, store):
     assert (cache.evict(b, w, 5000) == -1).all()
     same_pages(cache, want)
     assert torch.equal(w, w0) and lengths.tolist() == [100 + c for c in counts]
+
+
+# ---------------------------------------------------------------------------
+# paths that begin with negative entries
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("store,hk,dh", [("bf16", 1, 256), ("f32", 1, 64), ("fp8", 3, 64), ("bf16", 8, 128), ("int8", 2, 256)])
+@pytest.mark.parametrize("lead", [1, 5, 90])
+def test_accept_a_path_that_begins_below_the_rows(store, hk, dh, lead):
+    """Negative entries read as zeros, and the rows after them move up and then, past those left out, down: over many
+    steps, equal to a copy taken before.  Rows past the last one end the path."""
+    gen = torch.Generator().manual_seed(lead + dh)
+    news = [900, 700, 40, lead]
+    cu, lens, table, n_pages = pool(news, [n + 30 for n in news], 16, gen)
+    table[0, 5] = -1
+    cache, _, _ = filled(n_pages, hk, 16, dh, store, gen)
+    path = torch.full((4, 900), 7, dtype=torch.int32)
+    counts = []
+    for s, n in enumerate(news):
+        some = torch.randperm(n, generator=gen)[:n - lead // 2 if s == 1 else n // 2].sort().values.to(torch.int32)
+        mine = torch.cat([torch.arange(-lead, 0, dtype=torch.int32), some[:n - lead] if n > lead else some[:0]])
+        counts.append(min(n, len(mine)))
+        path[s, :counts[-1]] = mine[:counts[-1]]
+    path[2, counts[2] - 1] = 40
+    want = raw(cache)
+    new = ref.accept(want, cu.tolist(), lens.tolist(), table.numpy(), path.numpy(), counts)
+    b = batch(cu, lens, table)
+    cache.accept(b, path.to(DEV), i32(counts))
+    same_pages(cache, want)
+    assert b.tensors[1].tolist() == new
