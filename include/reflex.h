@@ -696,6 +696,18 @@ int reflex_paged_accept(const reflex_paged_cache* cache, const reflex_paged_batc
                         int32_t max_path, const int32_t* counts, int32_t* lengths_out, void* stream);
 
 /*
+ * The same for a memory whose keys are weighed (reflex_paged_weighed_attention):
+ * the accepted tokens' weights move with them, one that reads as zeros has weight
+ * 0, and the weights of the places that the other rows leave, tokens lengths[b] -
+ * n_b + c_b to lengths[b] - 1, become 0.  reflex_paged_accept leaves weights as
+ * they are: where rows were weighed before it, accepted tokens would have those of
+ * other rows, and the tokens that come next those of rows that were not accepted.
+ */
+int reflex_paged_weighed_accept(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const int32_t* path,
+                                int32_t max_path, const int32_t* counts, float* weights, int32_t* lengths_out,
+                                void* stream);
+
+/*
  * Attention that also adds up what every key got: reflex_paged_attention, and
  *   weights[slot of j][g] += sum over the batch's rows r that see token j, and
  *                            over the query heads h of g, of softmax_j(...)
@@ -704,8 +716,11 @@ int reflex_paged_accept(const reflex_paged_cache* cache, const reflex_paged_batc
  * order.  A row with zeros as its result adds nothing; one whose scores make its
  * result NaN adds NaN to all that it sees.  Pages whose weights are added to
  * belong to one sequence of the call: where they are shared, additions may be
- * lost.  A page that goes to another sequence needs its weights set to 0.  The
- * weights are the call's until its work is done.
+ * lost.  A weight belongs to the token in its slot: whoever gives a slot to another
+ * token (a page to another sequence, the place behind a length that was shortened
+ * to the token that comes next) sets it to 0; reflex_paged_weighed_accept and
+ * reflex_paged_evict do so for the places that they leave.  The weights are the
+ * call's until its work is done.
  * Errors: as reflex_paged_attention, with a workspace of its own size.
  */
 int reflex_paged_weighed_attention_workspace(const reflex_paged_cache* cache, const reflex_paged_batch* batch,

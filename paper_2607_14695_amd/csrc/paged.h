@@ -179,6 +179,7 @@ struct PagedAcceptArgs {
   const int32_t* path;    // [sequences][max_path]
   const int32_t* counts;  // [sequences]
   int max_path;
+  float* weights;         // [pages][heads][page size], moved too, or null
   int32_t* lengths;       // written; may be q.len
 };
 hipError_t launch_paged_accept(const PagedAcceptArgs& a, int elem_bytes, int scaled, hipStream_t s);

@@ -153,6 +153,18 @@ void fill_attention(PagedAttnArgs& a, const reflex_paged_cache* cache, const ref
 
 int done(hipError_t e) { return e == hipSuccess ? REFLEX_OK : hip_fail(e); }
 
+int accept_rows(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const int32_t* path, int32_t max_path,
+                const int32_t* counts, float* weights, int32_t* lengths, void* stream) {
+  RFX_CHECK(check_cache(cache));
+  RFX_CHECK(check_batch(batch, cache, 1));
+  RFX_CHECK(check_lists(cache, batch));
+  if (max_path < 0) return REFLEX_EINVAL;
+  if (batch->n_seqs == 0) return REFLEX_OK;
+  if ((max_path > 0 && !path) || !counts || !lengths) return REFLEX_EINVAL;
+  const PagedAcceptArgs a{pages_of(cache), seqs_of(batch), path, counts, max_path, weights, lengths};
+  return done(launch_paged_accept(a, elem_bytes(cache), cache->store >= REFLEX_STORE_FP8, reinterpret_cast<hipStream_t>(stream)));
+}
+
 }  // namespace
 
 extern "C" {
@@ -332,14 +344,13 @@ int reflex_paged_tree_attention(const reflex_paged_cache* cache, const reflex_pa
 
 int reflex_paged_accept(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const int32_t* path,
                         int32_t max_path, const int32_t* counts, int32_t* lengths, void* stream) {
-  RFX_CHECK(check_cache(cache));
-  RFX_CHECK(check_batch(batch, cache, 1));
-  RFX_CHECK(check_lists(cache, batch));
-  if (max_path < 0) return REFLEX_EINVAL;
-  if (batch->n_seqs == 0) return REFLEX_OK;
-  if ((max_path > 0 && !path) || !counts || !lengths) return REFLEX_EINVAL;
-  const PagedAcceptArgs a{pages_of(cache), seqs_of(batch), path, counts, max_path, lengths};
-  return done(launch_paged_accept(a, elem_bytes(cache), cache->store >= REFLEX_STORE_FP8, reinterpret_cast<hipStream_t>(stream)));
+  return accept_rows(cache, batch, path, max_path, counts, nullptr, lengths, stream);
+}
+
+int reflex_paged_weighed_accept(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const int32_t* path,
+                                int32_t max_path, const int32_t* counts, float* weights, int32_t* lengths, void* stream) {
+  if (batch && batch->n_seqs != 0 && (!weights || ((uintptr_t)weights & 3))) return REFLEX_EINVAL;
+  return accept_rows(cache, batch, path, max_path, counts, weights, lengths, stream);
 }
 
 int reflex_paged_weighed_attention_workspace(const reflex_paged_cache* cache, const reflex_paged_batch* batch,

@@ -145,16 +145,28 @@ __global__ __launch_bounds__(1024) void paged_accept_kernel(const PagedAcceptArg
     to = reinterpret_cast<uint4*>(base + (dst + hoff) * row_bytes + piece * 16);
     if (src >= 0) from = reinterpret_cast<const uint4*>(base + (src + hoff) * row_bytes + piece * 16);
   });
-  if (scaled) {
-    move_accepted<float, 1>(x.c, up, 2 * heads, [&](int i, int w, float*& to, const float*& from)
+  // the scales of K and V, and the weights: floats of every head
+  const int kinds = 2 * scaled + (a.weights != nullptr);
+  if (kinds) {
+    move_accepted<float, 1>(x.c, up, kinds * heads, [&](int i, int w, float*& to, const float*& from)
                             __attribute__((always_inline)) {
       int src, dst;
       places(i, src, dst);
       if (dst < 0 || src == dst) return;
-      float* const base = (w >= heads ? a.c.v_scale : a.c.k_scale) + ((int64_t)(h0 + w % heads) << a.c.shift);
+      const int kind = w / heads;
+      float* const all = kind == 2 * scaled ? a.weights : kind ? a.c.v_scale : a.c.k_scale;
+      float* const base = all + ((int64_t)(h0 + w - kind * heads) << a.c.shift);
       to = base + dst;
       if (src >= 0) from = base + src;
     });
+  }
+  if (a.weights) {  // the rows that were not accepted leave no weight (all that moves has been read)
+    const int64_t end = min(x.first + x.n, (int64_t)a.q.max_pages << a.c.shift);
+    for (int64_t j = max(x.first + x.c, (int64_t)0) + threadIdx.x; j < end; j += 1024) {
+      const int r = page_row(a.c, a.q, b, j);
+      if (r < 0) continue;
+      for (int h = h0; h < h0 + heads; ++h) a.weights[r + ((int64_t)h << a.c.shift)] = 0.f;
+    }
   }
   if (parts > 1) return;
   __syncthreads();  // every thread has read the length

@@ -311,16 +311,23 @@ class PagedCache:
               dt, self.head_dim ** -0.5 if scale is None else scale, *args, ws.data_ptr() if nb else None, nb)
         return out
 
-    def accept(self, batch: PagedBatch, path: torch.Tensor, counts: torch.Tensor) -> None:
+    def accept(self, batch: PagedBatch, path: torch.Tensor, counts: torch.Tensor,
+               weights: Optional[torch.Tensor] = None) -> None:
         """Go on from accepted drafted tokens: rows path[b][:counts[b]] of sequence b's rows (int32 [sequences, most]
         and [sequences], increasing) become the tokens behind the cached ones, and the batch's lengths end with
-        them, written where the batch's tensor holds them."""
+        them, written where the batch's tensor holds them.  ``weights`` (see ``attend``): if the drafted rows were
+        weighed, the accepted tokens' weights move with them and those of the other rows become 0; without it
+        weights stay as they are."""
         n = batch.c.n_seqs
         most = path.shape[1] if path.dim() == 2 else -1
         p = _index(path, (n, most), torch.int32, "path", self.device)
         c = _index(counts, (n,), torch.int32, "counts", self.device)
-        _call(self.device, "reflex_paged_accept", self.lib.reflex_paged_accept, self._ref, self._batch(batch),
-              p if most else None, most, c, batch.c.lengths)
+        args = (self._ref, self._batch(batch), p if most else None, most, c)
+        if weights is None:
+            _call(self.device, "reflex_paged_accept", self.lib.reflex_paged_accept, *args, batch.c.lengths)
+        else:
+            _call(self.device, "reflex_paged_weighed_accept", self.lib.reflex_paged_weighed_accept, *args,
+                  self._weights(weights), batch.c.lengths)
 
     def zero_weights(self) -> torch.Tensor:
         """A tensor for the weights of every key of the cache, of zeros."""

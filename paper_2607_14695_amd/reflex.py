@@ -160,6 +160,7 @@ def load_library() -> ctypes.CDLL:
         "reflex_paged_tree_attention": (c_i32, [P(PagedCacheC), P(PagedBatchC), P(RowsC), P(RowsC), c_i64, c_i32, c_i32,
                                                 c_f32, c_vp, c_i32, c_vp, ctypes.c_size_t, c_vp]),
         "reflex_paged_accept": (c_i32, [P(PagedCacheC), P(PagedBatchC), c_vp, c_i32, c_vp, c_vp, c_vp]),
+        "reflex_paged_weighed_accept": (c_i32, [P(PagedCacheC), P(PagedBatchC), c_vp, c_i32, c_vp, c_vp, c_vp, c_vp]),
         "reflex_paged_weighed_attention_workspace": (c_i32, [P(PagedCacheC), P(PagedBatchC), c_i64, c_i32, c_i32,
                                                              P(ctypes.c_size_t)]),
         "reflex_paged_weighed_attention": (c_i32, [P(PagedCacheC), P(PagedBatchC), P(RowsC), P(RowsC), c_i64, c_i32,

@@ -7,7 +7,8 @@ import torch
 from paper_2607_14695_amd.paged import PagedBatch
 
 from . import draft_reference as ref
-from .test_gpu_draft import raw, same_pages
+from . import paged_reference as pref
+from .test_gpu_draft import STORES, check_evict, check_weighed, raw, same_pages
 from .test_gpu_paged import DEV, batch, draw, filled, pool
 
 pytestmark = pytest.mark.gpu
@@ -77,3 +78,81 @@ def test_accept_a_path_that_begins_below_the_rows(store, hk, dh, lead):
     cache.accept(b, path.to(DEV), i32(counts))
     same_pages(cache, want)
     assert b.tensors[1].tolist() == new
+
+
+# ---------------------------------------------------------------------------
+# acceptance of rows that were weighed
+# ---------------------------------------------------------------------------
+def accept_weighed(pages, w, cu, lengths, table, path, counts):
+    """By definition: pages and weights [pages, kv heads, page size] changed in place; returns the new lengths."""
+    new = ref.accept([*pages, w], cu, lengths, table, path, counts)
+    for s, length in enumerate(lengths):
+        for j in range(new[s], length):
+            at = pref.place(table[s], w.shape[0], w.shape[2], j)
+            if at is not None:
+                w[at[0], :, at[1]] = 0
+    return new
+
+
+@pytest.mark.parametrize("store,hk,dh,ps", STORES)
+def test_accept_moves_weights(store, hk, dh, ps):
+    """Rows of every count, absent pages among them, a row past the last one, rows before the start."""
+    gen = torch.Generator().manual_seed(hk + 1)
+    news, lengths = [5, 1, 0, 40, 30, 7, 3, 300], [100, 1, 33, 90, 30, 4, 50, 310]
+    cu, lens, table, n_pages = pool(news, lengths, ps, gen, more_pages=1)
+    if ps < 64:
+        table[3, 70 // ps], table[4, 10 // ps], table[7, 200 // ps] = -1, n_pages, -1
+    cache, _, _ = filled(n_pages, hk, ps, dh, store, gen)
+    w = torch.rand(n_pages, hk, ps, generator=gen)
+    w.view(-1)[::7] = float("nan")
+    counts = [3, 0, 4, 33, 30, 5, -2, 150]
+    path = torch.full((8, 200), -5, dtype=torch.int32)
+    for s, n in enumerate(news):
+        c = min(max(counts[s], 0), n)
+        path[s, :c] = torch.randperm(n, generator=gen)[:c].sort().values
+    path[0, 2], path[7, :2] = 99, torch.tensor([-2, -1])
+    want, ww = raw(cache), w.numpy().copy()
+    new = accept_weighed(want, ww, cu.tolist(), lengths, table.numpy(), path.numpy(), counts)
+    b, w = batch(cu, lens, table), w.to(DEV)
+    cache.accept(b, path.to(DEV), i32(counts), weights=w)
+    same_pages(cache, want)
+    np.testing.assert_array_equal(w.cpu().numpy(), ww)
+    assert b.tensors[1].tolist() == new
+
+
+def test_accept_refuses_other_weights():
+    gen = torch.Generator().manual_seed(1)
+    cu, lens, table, n_pages = pool([2], [20], 8, gen)
+    cache, _, _ = filled(n_pages, 2, 8, 64, "bf16", gen)
+    b, good = batch(cu, lens, table), cache.zero_weights()
+    for bad in (good.double(), good[:1], good.transpose(0, 1), good.clone().requires_grad_(), good.cpu()):
+        with pytest.raises(ValueError):
+            cache.accept(b, i32([[0]]), i32([1]), weights=bad)
+    assert b.tensors[1].tolist() == [20]
+
+
+@pytest.mark.parametrize("dtype,store", [("bf16", "bf16"), ("f32", "int8")])
+def test_weighed_drafts_accepted_and_cut(dtype, store):
+    """Weighed rows, some of them accepted, more rows in the places of the others, and a cut: every token's weight is
+    what it got itself."""
+    gen = torch.Generator().manual_seed(23)
+    hk, heads, dh, ps, news = 2, 4, 64, 8, [12, 30]
+    cu, lens, table, n_pages = pool(news, [120, 77], ps, gen, more_pages=8)
+    table[table < 0] = n_pages + torch.arange(int((table < 0).sum()), dtype=torch.int32)
+    n_pages += table.numel()
+    cache, kk, vv = filled(n_pages, hk, ps, dh, store, gen)
+    w = check_weighed(draw(gen, (42, heads, dh), dtype), cache, (kk, vv), cu, lens, table, True, 0, dtype, gen,
+                      start=torch.zeros(n_pages, hk, ps))
+    path = torch.stack([torch.arange(1, 13, 2), torch.arange(4, 30, 5)]).to(torch.int32)
+    ww = w.cpu().numpy().copy()
+    pages = [kk, vv]
+    new = accept_weighed(pages, ww, cu.tolist(), lens.tolist(), table.numpy(), path.numpy(), [6, 4])
+    b = batch(cu, lens, table)
+    cache.accept(b, path.to(DEV), i32([6, 4]), weights=w)
+    np.testing.assert_array_equal(w.cpu().numpy(), ww)
+    assert b.tensors[1].tolist() == new
+    # the next rows, over places of rows that were not accepted
+    cu, lens = torch.tensor([0, 5, 9], dtype=torch.int32), torch.tensor([new[0] + 5, new[1] + 4], dtype=torch.int32)
+    w = check_weighed(draw(gen, (9, heads, dh), dtype), cache, pages, cu, lens, table, True, 0, dtype, gen,
+                      start=torch.from_numpy(ww))
+    check_evict(cache, w, lens, table, 60, 4, 9)
