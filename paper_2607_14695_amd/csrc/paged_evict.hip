@@ -253,7 +253,8 @@ __global__ __launch_bounds__(kMoveThreads) void paged_move_kernel(const PagedEvi
   const int col = blockIdx.x - (int)list * all;
   const int b = (int)(list / a.c.n_kv), g = (int)(list - (int64_t)b * a.c.n_kv);
   const int2 cut = a.cut[list];  // (length as it was given, length that is cut or 0)
-  if (g == 0 && col == all - 1 && threadIdx.x == 0) a.lengths[b] = cut.y ? a.keep : cut.x;
+  // (a length past the table may be longer than `keep` without a token to move)
+  if (g == 0 && col == all - 1 && threadIdx.x == 0) a.lengths[b] = min(cut.x, a.keep);
   if (!cut.y) return;
   const int32_t* const from = a.from + list * a.keep;
   const int64_t hoff = (int64_t)g << a.c.shift;

@@ -156,3 +156,24 @@ def test_weighed_drafts_accepted_and_cut(dtype, store):
     w = check_weighed(draw(gen, (9, heads, dh), dtype), cache, pages, cu, lens, table, True, 0, dtype, gen,
                       start=torch.from_numpy(ww))
     check_evict(cache, w, lens, table, 60, 4, 9)
+
+
+# ---------------------------------------------------------------------------
+# lengths past the table
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("keep", [64, 65, 80, 5000])
+def test_evict_with_a_budget_past_the_table(keep):
+    """Lengths become min(length, keep), whatever the table holds: four pages of 16 tokens, none of which moves."""
+    gen = torch.Generator().manual_seed(keep)
+    lengths = [100, 64, 63, 20000, 0, 80]
+    cu, _, table, n_pages = pool([0] * 6, [64] * 6, 16, gen)
+    cache, _, _ = filled(n_pages, 2, 16, 64, "fp8", gen)
+    want, w = raw(cache), torch.rand(n_pages, 2, 16, generator=gen).to(DEV)
+    w0, b = w.clone(), batch(cu, torch.tensor(lengths, dtype=torch.int32), table)
+    kept = cache.evict(b, w, keep, sinks=3, recent=9)
+    assert b.tensors[1].tolist() == [min(n, keep) for n in lengths]
+    for s, n in enumerate(lengths):
+        mine = list(range(min(n, 64)))
+        assert kept[s].tolist() == [mine + [-1] * (keep - len(mine))] * 2
+    same_pages(cache, want)
+    assert torch.equal(w, w0)
