@@ -657,7 +657,8 @@ int reflex_paged_attention(const reflex_paged_cache* cache, const reflex_paged_b
  * j is i or one of its ancestors.  parents: device int32 [n_rows], indexes among
  * the sequence's rows; what is not in [0, i) follows the cached tokens.
  * positions (device int64 [n_rows], may be NULL): lengths[b] - n_b + the number
- * of the row's ancestors, as reflex_paged_write takes them.  A row that the words
+ * of the row's ancestors, as reflex_paged_write takes them where lengths count all
+ * tokens; after reflex_paged_evict add those that were dropped.  A row that the words
  * cannot name sees no row and has the position of one without ancestors.  Rows of
  * no sequence keep what is there.  The page table is not used.  n_seqs <= 2^18.
  * Errors: REFLEX_EINVAL, REFLEX_EHIP.
@@ -738,7 +739,11 @@ int reflex_paged_weighed_attention(const reflex_paged_cache* cache, const reflex
  * kept tokens' K, V, scales and weights move to tokens 0 .. keep - 1 in their
  * order, the weights of the places that are left become 0, and lengths_out[b] is
  * min(lengths[b], keep).  Keys stay rotated by the positions that they were
- * written with.  A length counts up to max_pages * page_size.
+ * written with, while lengths then count places: rotary positions of later tokens
+ * are their index plus the number of tokens dropped so far, which the caller keeps
+ * (lengths before less lengths after) and adds to those of reflex_paged_tree, and
+ * hands to reflex_paged_write, whose own are the indexes; and a window of the
+ * attention is one of places.  A length counts up to max_pages * page_size.
  * kept (device int32 [n_seqs][n_kv_heads][keep], may be NULL): the tokens that
  * were kept, increasing; of a sequence that was not cut its own, then -1.
  * cu_rows is not read.  A kept token that is absent reads as zeros, with weight 0.

@@ -157,8 +157,9 @@ class PagedBatch:
         """(mask, positions) of drafted tokens: ``parents`` (int32 [rows]) names each row's parent among its
         sequence's rows, -1 for one that follows the cached tokens.  ``mask`` int64 [rows, words]: as bits the rows
         that each row sees, itself and its ancestors, for ``PagedCache.attend_tree``; ``positions`` int64 [rows] for
-        ``PagedCache.write`` and ``Rotary.apply``.  ``max_rows``: the most rows of a sequence (0: all rows), at most
-        4,096.  Without ``out``, rows of no sequence are undefined."""
+        ``PagedCache.write`` and ``Rotary.apply``, counted from the batch's lengths: of a sequence that
+        ``PagedCache.evict`` has cut, add the tokens that it lost.  ``max_rows``: the most rows of a sequence (0: all
+        rows), at most 4,096.  Without ``out``, rows of no sequence are undefined."""
         n = parents.shape[0] if parents.dim() == 1 else -1
         p = _index(parents, (n,), torch.int32, "parents", self.device)
         if out is None:
@@ -229,8 +230,8 @@ class PagedCache:
     def write(self, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor, rotary: Optional[Rotary] = None,
               positions: Optional[torch.Tensor] = None) -> None:
         """Write the batch's rows k, v [rows, kv heads, head dim] into their pages, the keys rotated first where a
-        plan is given: by ``positions``, or by each token's index in its sequence.  Rows for the same slot (sequences
-        that share the page) have to be equal."""
+        plan is given: by ``positions``, or by each token's index in its sequence (in one that was cut give them: see
+        ``evict``).  Rows for the same slot (sequences that share the page) have to be equal."""
         n = k.shape[0]
         if v.dtype != k.dtype:
             raise ValueError("k and v have one type")
@@ -344,7 +345,10 @@ class PagedCache:
         ``sinks``, its last ``recent`` and the others of greatest weight, moved together in order with their
         weights; the weights of the places that are left become 0, and the batch's lengths are written where its
         tensor holds them.  Returns ``kept`` (int32 [sequences, kv heads, keep]): the tokens that were kept, with -1
-        behind those of a shorter sequence.  Pages of the call's sequences are not shared."""
+        behind those of a shorter sequence.  Pages of the call's sequences are not shared.
+        Kept keys stay rotated by the positions that they were written with, and lengths then count places: rotary
+        positions of later tokens are their index plus the tokens dropped so far (lengths before less lengths after),
+        and a ``window`` is one of places."""
         for x, what in ((keep, "keep"), (sinks, "sinks"), (recent, "recent")):
             _int32(x, what)
         ref, w = self._batch(batch), self._weights(weights)

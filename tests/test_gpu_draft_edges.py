@@ -1,14 +1,17 @@
 """GPU checks of drafted tokens and a bounded memory where a call meets the edge of what its arguments allow: tables
-without pages, lengths past the table, paths below the rows."""
+without pages, lengths past the table, paths below the rows; weights and positions after a move."""
+import re
+from pathlib import Path
+
 import numpy as np
 import pytest
 import torch
 
-from paper_2607_14695_amd.paged import PagedBatch
+from paper_2607_14695_amd.paged import PagedBatch, PagedCache
 
 from . import draft_reference as ref
 from . import paged_reference as pref
-from .test_gpu_draft import STORES, check_evict, check_weighed, raw, same_pages
+from .test_gpu_draft import STORES, check_evict, check_weighed, random_parents, raw, same_pages
 from .test_gpu_paged import DEV, batch, draw, filled, pool
 
 pytestmark = pytest.mark.gpu
@@ -177,3 +180,45 @@ def test_evict_with_a_budget_past_the_table(keep):
         assert kept[s].tolist() == [mine + [-1] * (keep - len(mine))] * 2
     same_pages(cache, want)
     assert torch.equal(w, w0)
+
+
+# ---------------------------------------------------------------------------
+# positions after a cut
+# ---------------------------------------------------------------------------
+def test_the_readme_example_rotates_drafts_by_positions_of_the_uncut_sequence():
+    """The example run as it stands, over one memory that is cut and one that is not: drafted keys have the positions
+    that their tokens had without the cut, behind which the kept keys were rotated."""
+    gen = torch.Generator().manual_seed(29)
+    text = (Path(__file__).resolve().parent.parent / "README.md").read_text()
+    code = next(c for c in re.findall(r"```python\n(.*?)```", text, re.S) if "draft.tree" in c)
+    uncut, new, kept = [7100, 3000], [16, 9], [7000, 3000]
+    rows = sum(new)
+    n_pages = 200
+    table = torch.randperm(n_pages, generator=gen)[:196].view(2, 98).to(torch.int32)
+    table = torch.cat([table, torch.full((2, 20), -1, dtype=torch.int32)], 1)
+    table[0, 98:112], table[1, 60:74], table[1, 74:] = table[1, 60:74].clone(), -1, -1
+    cu, lengths = i32([0, new[0], rows]), i32(uncut)
+    k, v = (torch.randn(rows, 1, 256, generator=gen).bfloat16().to(DEV) for _ in range(2))
+    parents = random_parents(new, gen)
+    names = dict(
+        torch=torch, n_pages=n_pages, cu_rows=cu, lengths=lengths, page_table=table.to(DEV), rows=rows, k=k, v=v,
+        q=torch.randn(rows, 8, 256, generator=gen).bfloat16().to(DEV),
+        pos=torch.cat([torch.arange(u - n, u) for u, n in zip(uncut, new)]).expand(3, -1).contiguous().to(DEV),
+        draft=PagedBatch(cu, i32([a + b for a, b in zip(kept, new)]), table.to(DEV)), parents=parents.to(DEV),
+        sequence=torch.tensor([0] * new[0] + [1] * new[1], device=DEV),
+        path=torch.stack([torch.arange(1, 9, 2), torch.arange(2, 6)]).to(torch.int32).to(DEV), counts=i32([4, 3]))
+    exec(code, names)
+    assert lengths.tolist() == kept
+    sees, _ = ref.tree(parents.tolist(), cu.tolist(), uncut, 1, rows)
+    want = [uncut[int(r >= new[0])] + len(sees[r]) - 1 for r in range(rows)]
+    assert names["pos"].tolist() == want
+    # the accepted keys are those of their tokens, rotated by these positions
+    took = [1, 3, 5, 7, new[0] + 2, new[0] + 3, new[0] + 4]
+    ends = i32([a + c for a, c in zip(kept, (4, 3))])
+    assert names["draft"].tensors[1].tolist() == ends.tolist()
+    accepted = PagedBatch(i32([0, 4, 7]), ends, table.to(DEV))
+    other = PagedCache.zeros(n_pages, 64, 1, 256, torch.float8_e4m3fn)
+    other.write(accepted, names["k"][took], names["v"][took], rotary=names["rope"],
+                positions=torch.tensor(want, device=DEV)[took])
+    for x, y in zip(names["cache"].read(accepted, 7), other.read(accepted, 7)):
+        assert torch.equal(x, y)
