@@ -161,11 +161,13 @@ class PagedBatch:
         ``PagedCache.evict`` has cut, add the tokens that it lost.  ``max_rows``: the most rows of a sequence (0: all
         rows), at most 4,096.  Without ``out``, rows of no sequence are undefined."""
         n = parents.shape[0] if parents.dim() == 1 else -1
+        words = -(-(max_rows if max_rows > 0 else max(n, 1)) // 64)
+        if out is None and words > MAX_TREE_WORDS:
+            most = f"a sequence's tree has at most {64 * MAX_TREE_WORDS} rows"
+            raise ValueError(f"{most}, not {max_rows}" if max_rows > 0 else
+                             f"{most}: of {n} rows in all, give max_rows, the most that one has")
         p = _index(parents, (n,), torch.int32, "parents", self.device)
         if out is None:
-            words = -(-(max_rows if max_rows > 0 else max(n, 1)) // 64)
-            if not 1 <= words <= MAX_TREE_WORDS:
-                raise ValueError(f"a tree has at most {64 * MAX_TREE_WORDS} rows a sequence, not {max_rows or n}")
             mask = torch.empty((n, words), dtype=torch.int64, device=self.device)
             positions = torch.empty(n, dtype=torch.int64, device=self.device)
             m, pos = mask.data_ptr(), positions.data_ptr()

@@ -222,3 +222,15 @@ def test_the_readme_example_rotates_drafts_by_positions_of_the_uncut_sequence():
                 positions=torch.tensor(want, device=DEV)[took])
     for x, y in zip(names["cache"].read(accepted, 7), other.read(accepted, 7)):
         assert torch.equal(x, y)
+
+
+def test_trees_of_many_sequences_with_more_rows_together_than_one_may_have():
+    gen = torch.Generator().manual_seed(31)
+    news = [64] * 80 + [1]
+    n, parents = sum(news), random_parents(news, gen)
+    b = PagedBatch(i32([0] + list(np.cumsum(news))), i32([m + 9 for m in news]), torch.zeros(81, 0, dtype=torch.int32, device=DEV))
+    with pytest.raises(ValueError, match="give max_rows"):
+        b.tree(parents.to(DEV))
+    mask, pos = b.tree(parents.to(DEV), max_rows=64)
+    sees, want = ref.tree(parents.tolist(), [64 * s for s in range(81)] + [n], [m + 9 for m in news], 1, n)
+    assert mask[:, 0].tolist() == [ref.words_of(x, 1)[0] for x in sees] and pos.tolist() == want
