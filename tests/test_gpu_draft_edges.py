@@ -234,3 +234,61 @@ def test_trees_of_many_sequences_with_more_rows_together_than_one_may_have():
     mask, pos = b.tree(parents.to(DEV), max_rows=64)
     sees, want = ref.tree(parents.tolist(), [64 * s for s in range(81)] + [n], [m + 9 for m in news], 1, n)
     assert mask[:, 0].tolist() == [ref.words_of(x, 1)[0] for x in sees] and pos.tolist() == want
+
+
+# ---------------------------------------------------------------------------
+# other streams, and graphs
+# ---------------------------------------------------------------------------
+def test_a_side_stream_and_replays_leave_what_eager_calls_leave():
+    """A chain of all calls, weighed acceptance among them: on a side stream, and captured and replayed, the pages,
+    scales, weights, lengths and results are those of the same calls on the current stream."""
+    gen = torch.Generator().manual_seed(37)
+    news, ps = [20, 33], 8
+    cu, lens, table, n_pages = pool(news, [150, 260], ps, gen)
+
+    def made():
+        cache, _, _ = filled(n_pages, 2, ps, 64, "fp8", torch.Generator().manual_seed(5))
+        return cache, batch(cu, lens, table), cache.zero_weights()
+
+    q, parents = draw(gen, (53, 4, 64), "bf16").to(DEV), random_parents(news, gen).to(DEV)
+    path = torch.stack([torch.arange(1, 13, 2), torch.arange(0, 30, 5)]).to(torch.int32).to(DEV)
+    counts = i32([6, 4])
+
+    def step(cache, b, w):
+        mask, pos = b.tree(parents, max_rows=33)
+        outs = [mask, pos, cache.attend_tree(b, q, mask), cache.attend(b, q, weights=w)]
+        cache.accept(b, path, counts, weights=w)
+        return [*outs, cache.evict(b, w, 100, sinks=2, recent=10)]
+
+    def left(cache, b, w, outs):
+        return [t.view(torch.uint8) if t.element_size() == 1 else t
+                for t in (cache.k, cache.v, cache.k_scale, cache.v_scale, w, b.tensors[1], *outs)]
+
+    def same(one, two):
+        assert all(torch.equal(x, y) for x, y in zip(left(*one), left(*two)))
+
+    eager, aside, graphed = made(), made(), made()
+    first = [t.clone() for t in left(*eager, [])]
+    outs = step(*eager)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        outs_aside = step(*aside)
+    torch.cuda.synchronize()
+    same((*eager, outs), (*aside, outs_aside))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs_graphed = step(*graphed)
+    for turn in range(3):
+        for state in (eager, graphed):  # lengths come back, with what has become of pages and weights
+            state[1].tensors[1].copy_(lens - 7 * turn)
+        if turn == 0:
+            for state in (eager, graphed):
+                for t, f in zip(left(*state, []), first):
+                    t.copy_(f)
+        q.copy_(draw(gen, (53, 4, 64), "bf16"))
+        outs = step(*eager)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        same((*eager, outs), (*graphed, outs_graphed))
