@@ -670,7 +670,9 @@ int reflex_paged_tree(const reflex_paged_batch* batch, const int32_t* parents, i
  * Attention of drafted tokens: as reflex_paged_attention in each respect, with a
  * workspace of its own size, where row r sees the present tokens before its sequence's
  * rows (j < lengths[b] - n_b) and those of the sequence's rows that its bits
- * name.  A row may see nothing, itself included: then it gets zeros.
+ * name.  A row may see nothing, itself included: then it gets zeros.  Few rows are
+ * here also those of a batch with little work in all (16 bits of a probability,
+ * else 8 in bf16): a row's rounding may differ with the rows that it comes with.
  */
 int reflex_paged_tree_attention_workspace(const reflex_paged_cache* cache, const reflex_paged_batch* batch,
                                           int64_t n_rows, int32_t n_q_heads, int32_t dtype, size_t* bytes);

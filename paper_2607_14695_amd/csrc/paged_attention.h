@@ -353,8 +353,9 @@ RFX_DEV int count_tiles(const PagedAttnArgs& a, int bm, int lane) {
 // are not split alike: the batch's work (tiles x keys) is divided by the number of
 // workgroups that the chip holds, and every tile has as many splits, alike ones, as
 // that many keys to a split ask for.  32 ragged trees of 26 to 64 rows of 8 heads
-// of 256 over 3,344 to 15,409 fp8 keys take 242 us (505 TFLOP/s); with two splits
-// each they took 327, the longest ones' time.
+// of 256 over 3,344 to 15,409 fp8 keys take 228 us in a row of calls, with their
+// merge (530 TFLOP/s; by the profiler, which leaves pauses between the calls, 241
+// and 9); with two splits each they took 327 against 234, the longest ones' time.
 //
 // A unit is a tile's split; units are numbered over the sequences, in each over
 // the splits and in these over the tiles, which share the split's keys.
@@ -1036,8 +1037,11 @@ __global__ __launch_bounds__(256, (few_occupancy<T, ST, DH, MR>)) void paged_att
 // the 32x32x16 product.  A wave forms the scores of tile t + 1 while it takes
 // the softmax of tile t, so that its vector work runs under its matrix work;
 // K of tile t + 2 and V of tile t + 1 are on their way meanwhile, with one
-// barrier a tile.  The probabilities are rounded to bf16 once (two halves, as
-// with few rows, would double the second product).
+// barrier a tile.  The probabilities are rounded to bf16 once: two halves, as
+// with few rows, double the second product and bring the error against 64 bits
+// from 0.0023 to the 0.0017 of the result's own rounding (32 ragged trees over fp8
+// keys 228 and 269 us, 8 trees of 95 to 128 rows of 32 heads of 128 over 8,192 bf16
+// keys 160 and 203).
 //
 // Two prompts of 8,192 rows with 32 heads of 128, causal: 1.09-1.13 ms, 975-1,010
 // TFLOP/s, matrix units busy for 54 % and vector issue for 56 % of the cycles:

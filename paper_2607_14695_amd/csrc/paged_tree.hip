@@ -12,7 +12,8 @@ namespace {
 // words of a row are finished from the last to the first, and the walk ends; a
 // chain of 4,096 is the longest.  One workgroup to a sequence, whose parents
 // are held in LDS: the walk is a chain of LDS reads, the kernel all latency (16
-// rows 2.2 us, 64 trees of 78 to 256 rows 5 us, a launch among them).
+// rows 2.2 us, 64 trees of 78 to 256 rows 5 us, a launch among them; a chain's
+// walks are as long as it is: of 256 rows 26 us, of 1,024 255, of 4,096 3.6 ms).
 __global__ __launch_bounds__(256) void paged_tree_kernel(const PagedTreeArgs a) {
   __shared__ int32_t parent[kMaxTreeRows];
   const int b = blockIdx.x;
@@ -59,7 +60,7 @@ __global__ __launch_bounds__(256) void paged_tree_kernel(const PagedTreeArgs a) 
 // first to the last: either way a place is never read after a later step has
 // written it.  A step is some thousands of bytes, and is stored only when all of it
 // was read.  One workgroup to a sequence, which also writes its length (32
-// sequences of 6 tokens of one 256-wide head 3.7 us, a chain of latencies); where
+// sequences of 6 tokens of one 256-wide head 4 us, a chain of latencies); where
 // that would be many bytes, one to each `per_part` heads, and the lengths in a
 // launch of their own (8 sequences of up to 90 tokens of 8 heads of 128 took 31 us
 // in 8 workgroups).
@@ -208,8 +209,8 @@ hipError_t launch_paged_accept(const PagedAcceptArgs& a, int elem_bytes, int sca
 // 128: 128 rows of 256 over 833 keys 16 against 29, 512 rows over 3,000 keys 31
 // against 36, 8 times 32 rows of 128 over 8,192 keys 23 against 31; the other way
 // 8 times 128 rows of 256 over 3,000 keys 47 against 35, 8 times 128 rows of 128
-// over 8,192 keys 49 against 36).  How many workgroups share the batch's work;
-// and the splits that a tile can have at most, which the workspace has room for.
+// over 8,192 keys 49 against 36).  Their probabilities then have 16 bits.  How
+// many workgroups share the batch's work; and the splits that a tile can have at most, which the workspace has room for.
 PagedTreePlan paged_tree_plan(const reflex_paged_cache& c, const reflex_paged_batch& b, int64_t n_rows, int n_q, int dtype) {
   PagedTreePlan p;
   const int group = n_q / c.n_kv_heads;
