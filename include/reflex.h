@@ -692,7 +692,7 @@ int reflex_paged_tree_attention(const reflex_paged_cache* cache, const reflex_pa
  * path does not increase, what the accepted tokens hold is undefined.  Pages that
  * rows move in belong to one sequence of the call.  lengths_out may be the batch's
  * lengths; n_b is not cut to a number of rows here.  n_seqs * n_kv_heads <= 2^18,
- * in the two calls below too.
+ * in the calls below too.
  * Errors: REFLEX_EINVAL, REFLEX_EHIP.
  */
 int reflex_paged_accept(const reflex_paged_cache* cache, const reflex_paged_batch* batch, const int32_t* path,
